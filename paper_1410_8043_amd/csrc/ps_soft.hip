@@ -1,0 +1,1736 @@
+// Operators over a whole item table (include/ps_soft.h): softmax cross entropy and distillation
+// with the gradients of both tables, and each row's k best items.
+//
+// The mathematics.  With s_ij = x_i . w_j, both losses need, per row i, lse_i and the mean
+// o_i = sum_j p_ij w_j of the items under the row's softmax, and, per item j, the sum
+// c_j = sum_i a_i p_ij x_i with a_i the row's share of the gradient.  The targets add sparse
+// terms: their scores for the loss, coef w_j to dX_i and coef x_i to dW_j.  So there are two dense
+// passes of one shape (k_pass): an OWN table whose rows stay in registers, a STREAM table that goes
+// by in tiles of 32 rows; a tile's scores come from matrix instructions, the weights p' = 2^(score -
+// reference) stay in the registers where the next matrix instruction wants them, and that one
+// adds p' times the tile's rows to the own rows' sums.  Rows over items carry the running sum
+// of p' (the softmax's), items over rows know each row's lse already and multiply by a_i.
+//
+// Numbers.  Matrix instructions of 16-bit floats with 32-bit sums: a table is scaled by a power of two
+// so that its largest number lies in [2^13, 2^14) and is held as one plane of fp16 (bf16 and
+// f16 tables: exact for all numbers above 2^-28 of the largest) or as two, h = fp16(x), l =
+// fp16(x - h) (f32 tables: 22 bits, to 2^-38 of the largest below that), and products drop l*l
+// (2^-22).  The weights p' are held in two planes in both cases.  Sums over items and rows, running
+// maxima and log-sum-exps are fp32.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdint>
+#include <cstdio>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "ps_soft.h"
+
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kMaxK = 512;
+constexpr int kTile = 32;       // rows of a packed tile, and of a matrix instruction
+constexpr int kFrag = 512;      // halves of one fragment: 64 lanes x 8
+constexpr int kThreads = 256;
+constexpr int kPackBlocks = 8;  // blocks of 32 numbers that packing holds in LDS at once
+constexpr int kParts = 256;     // workgroups, and partial maxima, of each table's scan
+constexpr int kRowParts = 1024; // most workgroups, and partial maxima, of the row scan
+constexpr float kNone = -1e30f; // reference before the first tile: finite, so that 2^(-inf - kNone) is 0
+// p' = 2^(score - reference + kShift), and the reference follows the maximum when it is exceeded by more than
+// kLag: p' stays below 2^15, and a weight of 2^-17 of the largest keeps 22 bits
+constexpr float kShift = 7.f, kLag = 8.f;
+
+// ------------------------------------------------------------------ element types
+struct bf16_t { uint16_t u; };
+struct f16_t { _Float16 h; };
+__device__ inline float to_f(float v) { return v; }
+__device__ inline float to_f(bf16_t v) { return __uint_as_float(static_cast<uint32_t>(v.u) << 16); }
+__device__ inline float to_f(f16_t v) { return static_cast<float>(v.h); }
+__device__ inline void from_f(float v, float &o) { o = v; }
+__device__ inline void from_f(float v, bf16_t &o) {
+  const uint32_t u = __float_as_uint(v);
+  o.u = v != v ? 0x7fc0 : static_cast<uint16_t>((u + 0x7fff + ((u >> 16) & 1)) >> 16);  // to nearest, ties to even
+}
+__device__ inline void from_f(float v, f16_t &o) { o.h = static_cast<_Float16>(v); }
+
+// K numbers k0 .. k0+3 of a row as floats, zeros behind K; vec: the row starts at a multiple of 4 elements' bytes
+template <class T>
+__device__ inline f32x4 load4(const T *row, int k0, int K, bool vec) {
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (vec && k0 + 4 <= K) {
+    if constexpr (sizeof(T) == 4) {
+      o = *reinterpret_cast<const f32x4 *>(row + k0);
+    } else {
+      const u16x4 v = *reinterpret_cast<const u16x4 *>(row + k0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        T t;
+        __builtin_memcpy(&t, reinterpret_cast<const char *>(&v) + 2 * q, 2);
+        o[q] = to_f(t);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (k0 + q < K) o[q] = to_f(row[k0 + q]);
+  }
+  return o;
+}
+template <class T>
+__device__ inline void store4(T *row, int k0, int K, bool vec, f32x4 v) {
+  T t[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) from_f(v[q], t[q]);
+  if (vec && k0 + 4 <= K) {
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<f32x4 *>(row + k0) = v;
+    } else {
+      u16x4 o;
+      __builtin_memcpy(&o, t, 8);
+      *reinterpret_cast<u16x4 *>(row + k0) = o;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (k0 + q < K) row[k0 + q] = t[q];
+  }
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ inline float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+__device__ inline float block_max(float v, float *sh) {  // kThreads threads; sh: 4 floats
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
+// ------------------------------------------------------------------ targets
+// What a call's rows and targets become before the passes.  Entry e of the lists: key (its item, or
+// `items` where it is none), coef (v or q), cb (its share weight tau coef of the gradients), erow (its row).
+struct Targets {
+  int64_t n, entries;
+  int32_t items, k;  // k: entries per row without row_ptr
+  const int64_t *row_ptr;
+  const int32_t *item;
+  const float *value;        // xent
+  const float *score, *tlse; // distill
+  int64_t ldt;
+  float tau;
+  const float *weight;
+  int32_t *key, *erow;
+  float *coef, *cb;
+  int32_t *act;                          // [n] 0: masked
+  float *total, *extra, *share, *gw;     // [n] sum of coef; sum q log q (NaN: a bad row); gw total; weight tau
+  float *part;                           // [gridDim.x] largest |share|
+};
+
+__device__ inline bool row_range(const int64_t *row_ptr, int64_t entries, int32_t k, int64_t i, int64_t &b, int64_t &e) {
+  if (!row_ptr) {
+    b = i * k;
+    e = b + k;
+    return true;
+  }
+  b = row_ptr[i];
+  e = row_ptr[i + 1];
+  if (b < 0 || e < b || e > entries) {
+    b = e = 0;
+    return false;
+  }
+  return true;
+}
+
+__global__ __launch_bounds__(kThreads) void k_fill_keys(int32_t *key, int64_t entries, int32_t items) {
+  for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < entries; e += static_cast<int64_t>(gridDim.x) * kThreads)
+    key[e] = items;
+}
+
+// One wavefront per row.  Bound by the reads of the lists.
+template <bool Distill>
+__global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
+  __shared__ float sh[4];
+  const int lane = threadIdx.x & 63;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 4;
+  const float inf = __builtin_inff();
+  float most = 0.f;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < a.n; i += step) {
+    int64_t b, e;
+    bool bad = !row_range(a.row_ptr, a.entries, a.k, i, b, e);
+    const int64_t src = Distill ? i * a.ldt - b : 0;  // the lists' stride
+    const float w = a.weight ? a.weight[i] : 1.f;
+    bool live = false;
+    float top = -inf, den = 1.f;
+    for (int64_t x = b + lane; x < e; x += 64) {
+      const int32_t j = a.item[x + src];
+      if (j >= a.items) bad = true;
+      bool here = j >= 0 && j < a.items;
+      if constexpr (Distill) {
+        const float t = here ? a.score[x + src] : -inf;
+        here = here && !(t == -inf);
+        if (here) top = t != t ? t : fmaxf(top, t / a.tau);
+      }
+      live = live || here;
+    }
+    live = __any(live);
+    bad = __any(bad);
+    const bool act = live && w != 0.f;
+    float z = 0.f;  // log of the teacher's sum
+    if constexpr (Distill) {
+      if (act) {
+        if (a.tlse) {
+          z = a.tlse[i];
+        } else {
+          top = wave_max(top);
+          den = 0.f;
+          for (int64_t x = b + lane; x < e; x += 64) {
+            const int32_t j = a.item[x + src];
+            const float t = j >= 0 && j < a.items ? a.score[x + src] : -inf;
+            if (!(t == -inf)) den += expf(t / a.tau - top);
+          }
+          z = top + logf(wave_sum(den));
+        }
+      }
+    }
+    float total = 0.f, extra = 0.f;
+    const float gw = act ? w * a.tau : 0.f;
+    for (int64_t x = b + lane; x < e; x += 64) {
+      const int32_t j = a.item[x + src];
+      float c = 0.f;
+      bool here = act && j >= 0 && j < a.items;
+      if (here) {
+        if constexpr (Distill) {
+          const float t = a.score[x + src];
+          if (t == -inf) {
+            here = false;
+          } else {
+            const float lq = t / a.tau - z;
+            c = expf(lq);
+            extra += c == 0.f ? 0.f : c * lq;
+          }
+        } else {
+          c = a.value ? a.value[x] : 1.f;
+        }
+      }
+      a.key[x] = here ? j : a.items;
+      a.coef[x] = c;
+      if (a.cb) {
+        a.cb[x] = gw * c;
+        a.erow[x] = static_cast<int32_t>(i);
+      }
+      total += c;
+    }
+    total = wave_sum(total);
+    extra = wave_sum(extra);
+    const float share = gw * total;
+    most = fmaxf(most, fabsf(share) < inf ? fabsf(share) : 0.f);
+    if (lane == 0) {
+      a.act[i] = act;
+      a.total[i] = total;
+      a.extra[i] = bad ? __builtin_nanf("") : extra;
+      a.share[i] = share;
+      a.gw[i] = gw;
+    }
+  }
+  most = block_max(most, sh);
+  if (threadIdx.x == 0) a.part[blockIdx.x] = most;
+}
+
+// ------------------------------------------------------------------ packing
+template <class T>
+struct Table {
+  const T *p;
+  int64_t ld, rows;
+  bool vec;
+  const int32_t *act;  // rows that are read (NULL: all)
+};
+
+// Largest finite magnitude of each table, kParts partial maxima each
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_absmax(Table<T> x, Table<T> w, int32_t K, float *part) {
+  __shared__ float sh[4];
+  const bool second = blockIdx.x >= kParts;
+  const Table<T> t = second ? w : x;
+  const int blk = blockIdx.x - (second ? kParts : 0);
+  const int per = (K + 3) / 4;  // threads per row
+  float most = 0.f;
+  const int64_t all = t.rows * per;
+  for (int64_t q = static_cast<int64_t>(blk) * kThreads + threadIdx.x; q < all; q += static_cast<int64_t>(kParts) * kThreads) {
+    const int64_t r = q / per;
+    if (t.act && !t.act[r]) continue;
+    const f32x4 v = load4(t.p + r * t.ld, static_cast<int>(q - r * per) * 4, K, t.vec);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float m = fabsf(v[c]);
+      most = fmaxf(most, m < __builtin_inff() ? m : 0.f);
+    }
+  }
+  most = block_max(most, sh);
+  if (threadIdx.x == 0) part[blockIdx.x] = most;
+}
+
+__device__ inline int scale_exp(float most) {
+  if (!(most > 0.f)) return 0;
+  int e;
+  (void)frexpf(most, &e);  // most in [2^(e-1), 2^e)
+  return 14 - e;
+}
+
+// Scalars that the kernels share
+struct Scal {
+  int32_t ex, ew;  // x~ = x 2^ex, w~ = w 2^ew
+  float amax;      // a power of two >= every |share| (1 where all are 0)
+  float pad;
+};
+
+struct PackSide {
+  _Float16 *out;
+  int64_t stride;  // halves per tile
+  int32_t tiles;
+  bool turned;     // the turned fragments too
+};
+
+// A tile of 32 rows as fragments: for the scores, chunk c of 16 numbers, lane l holds row l%32, numbers
+// 16c + 8(l/32) ..+7; and turned, for the sums, rows 16q ..+15 and numbers 32b ..+31: lane l holds
+// number 32b + l%32 of the rows that the score instruction leaves in this lane's registers
+// 8q .. 8q+7, 16q + {4h ..+3, 8 + 4h ..+3} with h = l/32: so weights go from one matrix instruction to
+// the next without a move.  One workgroup per tile; bound by memory.
+template <class T, int NP>
+__global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackSide px, PackSide pw, int32_t K, int32_t k16,
+                                                   int32_t kd, const float *part, const float *row_part, int32_t row_parts,
+                                                   Scal *scal) {
+  extern __shared__ float tile[];  // [32][32 min(kd, kPackBlocks) + 1]
+  __shared__ float sh[4];
+  const bool second = static_cast<int32_t>(blockIdx.x) >= px.tiles;
+  const Table<T> t = second ? w : x;
+  const PackSide ps = second ? pw : px;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) - (second ? px.tiles : 0);
+  const float most = block_max(part[(second ? kParts : 0) + threadIdx.x], sh);
+  const int ex = scale_exp(most);
+  if (at == 0) {
+    if (threadIdx.x == 0) (second ? scal->ew : scal->ex) = ex;
+    if (!second) {
+      float m = 0.f;
+      for (int q = threadIdx.x; q < row_parts; q += kThreads) m = fmaxf(m, row_part[q]);
+      __syncthreads();
+      m = block_max(m, sh);
+      if (threadIdx.x == 0) scal->amax = m > 0.f ? ldexpf(1.f, 14 - scale_exp(m)) : 1.f;
+    }
+  }
+  _Float16 *out = ps.out + at * ps.stride;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int wide = min(kd, kPackBlocks), ld = wide * 32 + 1;
+  for (int b0 = 0; b0 < kd; b0 += wide) {  // 256 numbers at a time: 33 KB of LDS
+    const int nb = min(wide, kd - b0), per = nb * 8;  // float4s per row
+    __syncthreads();
+    for (int q = threadIdx.x; q < kTile * per; q += kThreads) {
+      const int r = q / per, k0 = (q - r * per) * 4;
+      const int64_t row = at * kTile + r;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (row < t.rows && b0 * 32 + k0 < K && (!t.act || t.act[row])) v = load4(t.p + row * t.ld, b0 * 32 + k0, K, t.vec);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tile[r * ld + k0 + c] = ldexpf(v[c], ex);
+    }
+    __syncthreads();
+    for (int c = 2 * b0 + wave; c < min(2 * (b0 + nb), k16); c += 4) {
+      h8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = tile[l32 * ld + (c - 2 * b0) * 16 + half * 8 + i];
+        hi[i] = static_cast<_Float16>(v);
+        lo[i] = static_cast<_Float16>(v - static_cast<float>(hi[i]));
+      }
+      *reinterpret_cast<h8 *>(out + (c * NP) * kFrag + lane * 8) = hi;
+      if constexpr (NP == 2) *reinterpret_cast<h8 *>(out + (c * NP + 1) * kFrag + lane * 8) = lo;
+    }
+    if (!ps.turned) continue;
+    for (int f = wave; f < 2 * nb; f += 4) {
+      const int q = f / nb, b = f - q * nb;
+      h8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = tile[(q * 16 + (i >> 2) * 8 + half * 4 + (i & 3)) * ld + b * 32 + l32];
+        hi[i] = static_cast<_Float16>(v);
+        lo[i] = static_cast<_Float16>(v - static_cast<float>(hi[i]));
+      }
+      _Float16 *to = out + (k16 + q * kd + b0 + b) * NP * kFrag + lane * 8;
+      *reinterpret_cast<h8 *>(to) = hi;
+      if constexpr (NP == 2) *reinterpret_cast<h8 *>(to + kFrag) = lo;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the dense passes
+struct PassArgs {
+  const _Float16 *own, *str;
+  int64_t own_stride, str_stride;  // halves per tile
+  int64_t own_rows, str_rows;
+  int32_t k16, kd, d0;             // chunks of 16 numbers, blocks of 32, the first block summed here
+  const float *rowvec;             // COL: per tile of 32 stream rows, 32 first values and 32 shares
+  const Scal *scal;
+  float scale;                     // log2(e) / tau
+  int64_t tiles_per_split;
+  float *m, *l, *o;                // [splits][own rows padded]: reference, sum of p', sums [..][32 kd]
+};
+
+__device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Rows over items (COL = false) or items over rows (COL = true).  A wavefront owns 32 rows.
+// Score instruction: stream rows x own rows, so a lane holds one own row (l%32) and 16 stream rows
+// 8(r/4) + 4h + r%4 of each tile.
+template <int NP, int KC, int DB, bool COL>
+__global__ __launch_bounds__(64) void k_pass(PassArgs a) {
+  const int lane = threadIdx.x, half = lane >> 5;
+  const int64_t own_tile = blockIdx.x, own_pad = static_cast<int64_t>(gridDim.x) * kTile;
+  const int64_t split = blockIdx.y;
+  const int64_t tiles = (a.str_rows + kTile - 1) / kTile;
+  const int64_t t0 = split * a.tiles_per_split, t1 = min(t0 + a.tiles_per_split, tiles);
+  const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
+  h8 q[KC][NP];
+  const _Float16 *own = a.own + own_tile * a.own_stride;
+#pragma unroll
+  for (int c = 0; c < KC; ++c)
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      q[c][p] = h8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (c < a.k16) q[c][p] = *reinterpret_cast<const h8 *>(own + (c * NP + p) * kFrag + lane * 8);
+    }
+  f32x16 o[DB > 0 ? DB : 1];
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+  float ref = kNone, sum = 0.f;
+  for (int64_t t = t0; t < t1; ++t) {
+    const _Float16 *st = a.str + t * a.str_stride;
+    f32x16 s;
+    float share[16];
+    if constexpr (COL) {
+      const float *rv = a.rowvec + t * 64;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(rv + g * 8 + half * 4);
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(rv + 32 + g * 8 + half * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[g * 4 + i] = v[i];
+          share[g * 4 + i] = u[i];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    }
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      if (c < a.k16) {
+        const h8 h = *reinterpret_cast<const h8 *>(st + (c * NP) * kFrag + lane * 8);
+        s = mfma(h, q[c][0], s);
+        if constexpr (NP == 2) {
+          const h8 l = *reinterpret_cast<const h8 *>(st + (c * NP + 1) * kFrag + lane * 8);
+          s = mfma(h, q[c][1], s);
+          s = mfma(l, q[c][0], s);
+        }
+      }
+    }
+    if constexpr (!COL) {
+      if ((t + 1) * kTile > a.str_rows) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.str_rows) s[r] = -__builtin_inff();
+      }
+    }
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(top, __shfl_xor(top, 32)) * sc;
+    if (__any(top > ref + kLag)) {
+      const float to = top > ref + kLag ? top : ref;
+      const float down = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      sum *= down;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= down;
+    }
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, kShift - ref));
+      if constexpr (COL) {
+        p[r] *= share[r];
+        // the product and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
+        // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
+        asm("" : "+v"(p[r]));
+      }
+      if constexpr (!COL) sum += p[r];
+    }
+    if constexpr (DB > 0) {
+      const _Float16 *turned = st + a.k16 * NP * kFrag;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        h8 ph, pl;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          ph[i] = static_cast<_Float16>(p[8 * k + i]);
+          pl[i] = static_cast<_Float16>(fmaf(static_cast<float>(ph[i]), -1.f, p[8 * k + i]));
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          if (a.d0 + b < a.kd) {
+            const _Float16 *f = turned + ((k * a.kd + a.d0 + b) * NP) * kFrag + lane * 8;
+            const h8 h = *reinterpret_cast<const h8 *>(f);
+            o[b] = mfma(h, ph, o[b]);
+            o[b] = mfma(h, pl, o[b]);
+            if constexpr (NP == 2) o[b] = mfma(*reinterpret_cast<const h8 *>(f + kFrag), ph, o[b]);
+          }
+        }
+      }
+    }
+  }
+  const int64_t row = split * own_pad + own_tile * kTile + (lane & 31);
+  if (a.d0 == 0) {
+    sum += __shfl_xor(sum, 32);
+    if (half == 0) {
+      a.m[row] = ref;
+      if constexpr (!COL) a.l[row] = sum;
+    }
+  }
+  if constexpr (DB > 0) {
+    float *to = a.o + row * (a.kd * 32) + a.d0 * 32 + half * 4;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+      if (a.d0 + b < a.kd) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4 *>(to + b * 32 + g * 8) = f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
+      }
+  }
+}
+
+// ------------------------------------------------------------------ rows: join, targets, loss, dX
+// Lanes of a group hold a row: number k = v 4G + 4g + q at lane g, vector v, element q
+template <class T, int G, int V>
+__device__ inline void load_row(f32x4 (&x)[V], const T *row, int g, int K, bool vec) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = load4(row, v * 4 * G + 4 * g, K, vec);
+}
+
+template <class T>
+struct RowArgs {
+  int64_t n, entries, own_pad;
+  int32_t K, ldo, k, splits, items;
+  const int64_t *row_ptr;
+  Table<T> x, w;
+  const int32_t *key;
+  const float *coef, *total, *extra, *share, *gw;
+  const Scal *scal;
+  const float *m, *l, *o;
+  float scale, inv_tau, gain;
+  float *loss, *lse;
+  T *dX;
+  int64_t lddx;
+  bool vec_out;
+  float *rowvec;  // NULL: no pass over rows follows
+};
+
+// TW wavefronts per row (4: few rows with long lists).  Gathers of the target items' rows bound it.
+template <class T, int G, int V, int TW, bool DX>
+__global__ __launch_bounds__(kThreads) void k_row_finish(RowArgs<T> a) {
+  constexpr int NG = TW * 64 / G;  // groups per row
+  constexpr int RF = 4;            // rows in flight per group
+  __shared__ float part[TW == 4 ? 4 : 1][TW == 4 ? 64 * 4 * V + 1 : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int g = lane & (G - 1);
+  const int grp = (TW == 4 ? wave * (64 / G) : 0) + lane / G;
+  const int64_t i = TW == 4 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
+  const int64_t row_end = (a.n + kTile - 1) / kTile * kTile;
+  if (i >= a.n) {  // rows behind the last, to the end of its tile: no weight in the pass over rows
+    if (a.rowvec && i < row_end && lane == 0 && (TW == 1 || wave == 0)) {
+      a.rowvec[(i >> 5) * 64 + (i & 31)] = -__builtin_inff();
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = 0.f;
+    }
+    return;
+  }
+  float top = kNone;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.m[s * a.own_pad + i]);
+  float den = 0.f;
+  for (int s = 0; s < a.splits; ++s)
+    den += a.l[s * a.own_pad + i] * __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
+  const float lse2 = top - kShift + log2f(den);
+  const float lse = lse2 * 0.69314718055994530942f;
+  const bool act = !a.x.act || a.x.act[i];
+  f32x4 x[V], acc[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (act) load_row<T, G, V>(x, a.x.p + i * a.x.ld, g, a.K, a.x.vec);
+  float loss = 0.f;
+  int64_t b, e;
+  row_range(a.row_ptr, a.entries, a.k, i, b, e);
+  if (act) {
+    for (int64_t q = b + grp; q < e; q += NG * RF) {
+      int32_t key[RF];
+      float c[RF];
+      f32x4 y[RF][V];
+#pragma unroll
+      for (int f = 0; f < RF; ++f) {
+        const int64_t at = q + f * NG;
+        key[f] = at < e ? a.key[at] : a.items;
+        c[f] = at < e ? a.coef[at] : 0.f;
+      }
+#pragma unroll
+      for (int f = 0; f < RF; ++f) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (key[f] < a.items) load_row<T, G, V>(y[f], a.w.p + key[f] * a.w.ld, g, a.K, a.w.vec);
+      }
+#pragma unroll
+      for (int f = 0; f < RF; ++f) {
+        float d = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) d = fmaf(x[v][z], y[f][v][z], d);
+#pragma unroll
+        for (int s = G / 2; s > 0; s >>= 1) d += __shfl_xor(d, s);
+        if (key[f] < a.items) loss = fmaf(c[f], lse - d * a.inv_tau, loss);
+        if constexpr (DX) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) acc[v][z] = fmaf(c[f], y[f][v][z], acc[v][z]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int s = G; s < 64; s <<= 1) {
+    loss += __shfl_xor(loss, s);
+    if constexpr (DX) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) acc[v][z] += __shfl_xor(acc[v][z], s);
+    }
+  }
+  if constexpr (TW == 4) {
+    if (lane < G) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) part[wave][(v * 4 + z) * 64 + g] = acc[v][z];
+      if (g == 0) part[wave][64 * 4 * V] = loss;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    loss = part[0][64 * 4 * V] + part[1][64 * 4 * V] + part[2][64 * 4 * V] + part[3][64 * 4 * V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const int at = (v * 4 + z) * 64 + g;
+        acc[v][z] = part[0][at] + part[1][at] + part[2][at] + part[3][at];
+      }
+  }
+  if (lane == 0) {
+    if (a.loss) a.loss[i] = a.gain * (loss + a.extra[i]);
+    if (a.lse) a.lse[i] = lse;
+    if (a.rowvec) {
+      const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
+      a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 / sc : -__builtin_inff();
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.share[i] / a.scal->amax : 0.f;
+    }
+  }
+  if constexpr (DX) {
+    if (lane >= G) return;
+    const float gw = a.gw[i], mean = a.total[i] / den;
+    f32x4 o[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k0 = v * 4 * G + 4 * g;
+      o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k0 >= a.K) continue;
+      for (int s = 0; s < a.splits; ++s) {
+        const float f = __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(a.o + (s * a.own_pad + i) * a.ldo + k0);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) o[v][z] = fmaf(u[z], f, o[v][z]);
+      }
+      f32x4 d;
+#pragma unroll
+      for (int z = 0; z < 4; ++z) d[z] = act ? gw * (mean * ldexpf(o[v][z], -a.scal->ew) - acc[v][z]) : 0.f;
+      store4(a.dX + i * a.lddx, k0, a.K, a.vec_out, d);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the targets by item
+// A stable sort of the entries by item, 9 bits a pass: entries of an item stay in row order, so the
+// sums below have a fixed order.  A workgroup takes 4096 entries, a wavefront 1024 of them in order;
+// the rank of an entry among its wavefront's equal digits comes from the lanes' ballots.
+constexpr int kBits = 9, kBins = 1 << kBits, kSortTile = 4096;
+
+__global__ __launch_bounds__(kThreads) void k_sort_count(const int32_t *key, int64_t n, int shift, int32_t *hist, int32_t blocks) {
+  __shared__ int32_t cnt[kBins];
+  for (int b = threadIdx.x; b < kBins; b += kThreads) cnt[b] = 0;
+  __syncthreads();
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile;
+  for (int q = threadIdx.x; q < kSortTile; q += kThreads)
+    if (base + q < n) atomicAdd(&cnt[(key[base + q] >> shift) & (kBins - 1)], 1);
+  __syncthreads();
+  for (int b = threadIdx.x; b < kBins; b += kThreads) hist[static_cast<int64_t>(b) * blocks + blockIdx.x] = cnt[b];
+}
+
+// Exclusive sums of each digit's counts over the workgroups, and the digit's total
+__global__ __launch_bounds__(kThreads) void k_sort_scan(int32_t *hist, int32_t blocks, int32_t *total) {
+  __shared__ int32_t sh[4], carry;
+  int32_t *h = hist + static_cast<int64_t>(blockIdx.x) * blocks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) carry = 0;
+  for (int base = 0; base < blocks; base += kThreads) {
+    const int at = base + threadIdx.x;
+    const int32_t v = at < blocks ? h[at] : 0;
+    int32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int32_t u = __shfl_up(s, o);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) sh[wave] = s;
+    __syncthreads();
+    int32_t before = carry;
+    for (int w = 0; w < wave; ++w) before += sh[w];
+    if (at < blocks) h[at] = before + s - v;
+    __syncthreads();
+    if (threadIdx.x == kThreads - 1) carry = before + s;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) total[blockIdx.x] = carry;
+}
+
+struct Entries {
+  int32_t *key, *row;
+  float *cb;
+};
+__global__ __launch_bounds__(kThreads) void k_sort_move(Entries in, Entries out, int64_t n, int shift, const int32_t *hist,
+                                                        int32_t blocks, const int32_t *total) {
+  __shared__ int32_t cnt[4][kBins], sh[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / 4);
+  for (int b = threadIdx.x; b < 4 * kBins; b += kThreads) (&cnt[0][0])[b] = 0;
+  __syncthreads();
+  for (int q = lane; q < kSortTile / 4; q += 64)
+    if (base + q < n) atomicAdd(&cnt[wave][(in.key[base + q] >> shift) & (kBins - 1)], 1);
+  // where each digit starts: the digits before it, two per thread
+  const int b0 = 2 * threadIdx.x;
+  const int32_t v0 = total[b0], v1 = total[b0 + 1];
+  int32_t s = v0 + v1;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t u = __shfl_up(s, o);
+    if (lane >= o) s += u;
+  }
+  if (lane == 63) sh[wave] = s;
+  __syncthreads();
+  int32_t before = s - v0 - v1;
+  for (int w = 0; w < wave; ++w) before += sh[w];
+#pragma unroll
+  for (int z = 0; z < 2; ++z) {
+    int32_t at = before + (z ? v0 : 0) + hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x];
+    for (int w = 0; w < 4; ++w) {
+      const int32_t c = cnt[w][b0 + z];
+      cnt[w][b0 + z] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  volatile int32_t *mine = cnt[wave];
+  for (int q = lane; q < kSortTile / 4; q += 64) {
+    const bool in_range = base + q < n;
+    const int32_t key = in_range ? in.key[base + q] : 0;
+    const int d = (key >> shift) & (kBins - 1);
+    unsigned long long same = __ballot(in_range);
+#pragma unroll
+    for (int bit = 0; bit < kBits; ++bit) {
+      const unsigned long long set = __ballot((d >> bit) & 1);
+      same &= (d >> bit) & 1 ? set : ~set;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    if (in_range) {
+      const int32_t to = mine[d] + rank;
+      out.key[to] = key;
+      out.row[to] = in.row[base + q];
+      out.cb[to] = in.cb[base + q];
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (in_range && rank == 0) mine[d] += __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <class T>
+struct ItemArgs {
+  int64_t own_pad, entries, chunk, chunks;  // chunk: entries that one lane group sums
+  int32_t items, K, ldo, splits, kd;
+  Table<T> x;
+  Entries ent;
+  float *part;  // [2 chunks][32 kd] sums of a chunk's first and last item
+  float *ysum;  // [items][32 kd] sums of items whose entries lie inside one chunk
+  const Scal *scal;
+  const float *m, *o;
+  T *dW;
+  int64_t lddw;
+  bool vec_out;
+};
+
+// sum cb x_row of every item's entries, the sorted list cut into chunks: a chunk's first and last item may go on
+// in the neighbours, so their sums are kept apart.  Bound by the gathers of x rows.
+template <class T, int G, int V>
+__global__ __launch_bounds__(kThreads) void k_item_lists(ItemArgs<T> a) {
+  constexpr int RF = 4;
+  const int g = threadIdx.x & (G - 1);
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * (kThreads / G) + threadIdx.x / G;
+  if (c >= a.chunks) return;
+  const int64_t b = c * a.chunk, e = min(b + a.chunk, a.entries);
+  const int ld = a.kd * 32;
+  f32x4 acc[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int32_t cur = a.ent.key[b];
+  bool first = true;
+  auto put = [&](float *to) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k0 = v * 4 * G + 4 * g;
+      if (k0 < ld) *reinterpret_cast<f32x4 *>(to + k0) = acc[v];
+      acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  for (int64_t q = b; q < e; q += RF) {
+    int32_t key[RF];
+    float cb[RF];
+    f32x4 x[RF][V];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+      const bool in = q + f < e;
+      key[f] = in ? a.ent.key[q + f] : a.items;
+      cb[f] = in && key[f] < a.items ? a.ent.cb[q + f] : 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (in && key[f] < a.items) load_row<T, G, V>(x[f], a.x.p + a.ent.row[q + f] * a.x.ld, g, a.K, a.x.vec);
+    }
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+      if (q + f < e && key[f] != cur) {
+        if (first) {
+          put(a.part + 2 * c * ld);
+          first = false;
+        } else {
+          put(a.ysum + static_cast<int64_t>(cur) * ld);
+        }
+        cur = key[f];
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) acc[v][z] = fmaf(cb[f], x[f][v][z], acc[v][z]);
+    }
+  }
+  put(a.part + (2 * c + (first ? 0 : 1)) * ld);
+}
+
+__device__ inline int64_t lower(const int32_t *key, int64_t n, int32_t j) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (key[mid] < j) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+// dW_j: the passes' pieces joined, minus the targets' sums
+template <class T, int G, int V>
+__global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
+  const int g = threadIdx.x & (G - 1);
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * (kThreads / G) + threadIdx.x / G;
+  if (j >= a.items) return;
+  const int ld = a.kd * 32;
+  f32x4 o[V], y[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) o[v] = y[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto add = [&](f32x4 (&to)[V], const float *from, float f) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int k0 = v * 4 * G + 4 * g;
+      if (k0 >= ld) continue;
+      const f32x4 u = *reinterpret_cast<const f32x4 *>(from + k0);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) to[v][z] = fmaf(u[z], f, to[v][z]);
+    }
+  };
+  for (int s = 0; s < a.splits; ++s)
+    add(o, a.o + (s * a.own_pad + j) * a.ldo, __builtin_amdgcn_exp2f(a.m[s * a.own_pad + j] - kShift));
+  if (a.entries > 0) {
+    const int64_t lo = lower(a.ent.key, a.entries, static_cast<int32_t>(j)), hi = lower(a.ent.key, a.entries, static_cast<int32_t>(j) + 1);
+    if (hi > lo) {
+      const int64_t c0 = lo / a.chunk, c1 = (hi - 1) / a.chunk;
+      const bool from_start = lo == c0 * a.chunk;
+      if (c0 == c1 && !from_start && hi != min((c0 + 1) * a.chunk, a.entries)) {
+        add(y, a.ysum + j * ld, 1.f);
+      } else {
+        add(y, a.part + (2 * c0 + (from_start ? 0 : 1)) * ld, 1.f);
+#pragma unroll 4
+        for (int64_t c = c0 + 1; c <= c1; ++c) add(y, a.part + 2 * c * ld, 1.f);
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    f32x4 d;
+    const int k0 = v * 4 * G + 4 * g;
+    if (k0 >= a.K) continue;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) d[z] = (a.splits ? ldexpf(o[v][z], -a.scal->ex) * a.scal->amax : 0.f) - y[v][z];
+    store4(a.dW + j * a.lddw, k0, a.K, a.vec_out, d);
+  }
+}
+
+// ------------------------------------------------------------------ the best items
+// Scores in 64 bits, as keys whose unsigned order is that of the numbers; a workgroup keeps the best of what
+// it has seen in LDS: what beats the k-th best so far is put behind, and when the room is full it is
+// sorted and cut to k again.
+constexpr int kTopRoom = 2048;
+constexpr int kMaxTop = 256;
+
+__device__ inline uint64_t order_key(double v) {
+  if (v != v) return ~0ull;  // NaN above all
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v + 0.0));  // -0 as 0
+  return u >> 63 ? ~u : u | (1ull << 63);
+}
+__device__ inline double key_value(uint64_t k) {
+  return __longlong_as_double(static_cast<long long>(k >> 63 ? k & ~(1ull << 63) : ~k));
+}
+
+struct Best {
+  uint64_t *key;  // [kTopRoom]
+  int32_t *item;  // [kTopRoom]
+  int32_t *count;
+};
+__device__ inline bool before(uint64_t ka, int32_t ia, uint64_t kb, int32_t ib) { return ka > kb || (ka == kb && ia < ib); }
+
+// The room's first `count` entries in order, all threads; at most k of them stay.  Returns the k-th key (0: fewer).
+__device__ inline uint64_t best_cut(Best b, int k) {
+  __syncthreads();
+  const int n = *b.count;
+  int size = 2;
+  while (size < n) size <<= 1;
+  for (int q = n + threadIdx.x; q < size; q += kThreads) {
+    b.key[q] = 0;
+    b.item[q] = 0x7fffffff;
+  }
+  __syncthreads();
+  for (int len = 2; len <= size; len <<= 1)
+    for (int d = len >> 1; d > 0; d >>= 1) {
+      for (int q = threadIdx.x; q < size / 2; q += kThreads) {
+        const int lo = ((q & ~(d - 1)) << 1) | (q & (d - 1)), hi = lo | d;
+        const bool up = (lo & len) == 0;
+        const uint64_t ka = b.key[lo], kb = b.key[hi];
+        const int32_t ia = b.item[lo], ib = b.item[hi];
+        if (before(kb, ib, ka, ia) == up) {
+          b.key[lo] = kb; b.key[hi] = ka;
+          b.item[lo] = ib; b.item[hi] = ia;
+        }
+      }
+      __syncthreads();
+    }
+  if (threadIdx.x == 0) *b.count = min(n, k);
+  __syncthreads();
+  return n >= k ? b.key[k - 1] : 0;
+}
+
+// Every thread may bring one entry; entries come with increasing items or all differ
+__device__ inline void best_add(Best b, int k, bool want, uint64_t key, int32_t item, uint64_t &least) {
+  if (want && key >= least) {
+    const int at = atomicAdd(b.count, 1);
+    b.key[at] = key;
+    b.item[at] = item;
+  }
+  __syncthreads();
+  if (*b.count > kTopRoom - kThreads) least = best_cut(b, k);
+  __syncthreads();
+}
+
+template <class T>
+struct TopArgs {
+  int64_t row0, n;  // rows of this launch
+  int32_t items, K, k, words;
+  Table<T> x, w;
+  const uint32_t *excluded;  // [n][words] bits (NULL: none)
+  int64_t per_piece;
+  int32_t pieces;
+  uint64_t *key;   // [n][pieces][k]
+  int32_t *item;
+  int32_t *out_item;
+  float *out_score;
+  int64_t ldo;
+};
+
+template <class T>
+__device__ inline double dot64(const double *x, const T *w, int K, bool vec) {
+  double s = 0.0;
+  for (int k = 0; k < K; k += 4) {
+    const f32x4 v = load4(w, k, K, vec);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);  // products are exact
+  }
+  return s;
+}
+
+// The k best of a piece of the items for one row: an item per thread
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_top_scan(TopArgs<T> a) {
+  __shared__ double x[kMaxK];
+  __shared__ uint64_t keys[kTopRoom];
+  __shared__ int32_t items[kTopRoom], count;
+  const int64_t r = blockIdx.x;
+  const int piece = blockIdx.y;
+  const T *xr = a.x.p + (a.row0 + r) * a.x.ld;
+  for (int k = threadIdx.x; k < kMaxK; k += kThreads) x[k] = k < a.K ? static_cast<double>(to_f(xr[k])) : 0.0;
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  const Best b{keys, items, &count};
+  uint64_t least = 0;
+  const int64_t j0 = piece * a.per_piece, j1 = min(j0 + a.per_piece, static_cast<int64_t>(a.items));
+  for (int64_t base = j0; base < j1; base += kThreads) {
+    const int64_t j = base + threadIdx.x;
+    bool want = j < j1;
+    if (want && a.excluded) want = !((a.excluded[r * a.words + (j >> 5)] >> (j & 31)) & 1);
+    uint64_t key = 0;
+    if (want) key = order_key(dot64(x, a.w.p + j * a.w.ld, a.K, a.w.vec));
+    best_add(b, a.k, want, key, static_cast<int32_t>(j), least);
+  }
+  best_cut(b, a.k);
+  const int64_t to = (r * a.pieces + piece) * a.k;
+  for (int q = threadIdx.x; q < a.k; q += kThreads) {
+    a.key[to + q] = q < count ? keys[q] : 0;
+    a.item[to + q] = q < count ? items[q] : -1;
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_top_join(TopArgs<T> a) {
+  __shared__ uint64_t keys[kTopRoom];
+  __shared__ int32_t items[kTopRoom], count;
+  const int64_t r = blockIdx.x;
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  const Best b{keys, items, &count};
+  uint64_t least = 0;
+  const int64_t from = r * a.pieces * a.k, all = static_cast<int64_t>(a.pieces) * a.k;
+  for (int64_t base = 0; base < all; base += kThreads) {
+    const int64_t q = base + threadIdx.x;
+    const int32_t j = q < all ? a.item[from + q] : -1;
+    best_add(b, a.k, j >= 0, q < all ? a.key[from + q] : 0, j, least);
+  }
+  best_cut(b, a.k);
+  const int64_t to = (a.row0 + r) * a.ldo;
+  for (int q = threadIdx.x; q < a.k; q += kThreads) {
+    a.out_item[to + q] = q < count ? items[q] : -1;
+    a.out_score[to + q] = q < count ? static_cast<float>(key_value(keys[q])) : -__builtin_inff();
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void k_clear(uint32_t *p, int64_t n) {
+  for (int64_t q = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; q < n; q += static_cast<int64_t>(gridDim.x) * kThreads)
+    p[q] = 0;
+}
+// a bit per excluded item; one wavefront per row
+__global__ __launch_bounds__(kThreads) void k_exclude(const int64_t *row_ptr, const int32_t *item, int64_t entries, int64_t row0,
+                                                      int64_t n, int32_t items, int32_t words, uint32_t *bits) {
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  int64_t b, e;
+  row_range(row_ptr, entries, 0, row0 + r, b, e);
+  for (int64_t q = b + (threadIdx.x & 63); q < e; q += 64) {
+    const int32_t j = item[q];
+    if (j >= 0 && j < items) atomicOr(&bits[r * words + (j >> 5)], 1u << (j & 31));
+  }
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ the handle
+struct ps_soft {
+  int64_t items = 0;
+  int32_t K = 0, type = 0;
+  int32_t splits = 0;
+  int device = -1;
+  bool opened = false;
+  hipStream_t stream = nullptr;  // NULL: HIP's null stream
+  hipEvent_t moved = nullptr;
+  char *work = nullptr;
+  int64_t work_bytes = 0;
+  bool captured = false;
+  std::vector<void *> kept;  // workspaces that a captured graph may hold
+  std::string err;
+};
+
+namespace {
+
+int fail(ps_soft_t *h, int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    h->err = buf;
+  } catch (const std::bad_alloc &) {
+  }
+  return code;
+}
+
+#define SOFT_TRY(h, expr)                                                                                      \
+  do {                                                                                                        \
+    const hipError_t e_ = (expr);                                                                             \
+    if (e_ != hipSuccess) {                                                                                   \
+      (void)hipGetLastError();                                                                                \
+      return fail(h, e_ == hipErrorOutOfMemory ? PS_SOFT_ENOMEM : PS_SOFT_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
+    }                                                                                                         \
+  } while (0)
+
+// The caller's device comes back when the call returns
+struct DeviceGuard {
+  int before = -1;
+  ~DeviceGuard() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+int open(ps_soft_t *h, DeviceGuard &guard) {
+  int dev = 0;
+  SOFT_TRY(h, hipGetDevice(&dev));
+  if (h->device < 0) h->device = dev;
+  if (h->device != dev) {
+    const hipError_t e = hipSetDevice(h->device);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(h, PS_SOFT_EDEVICE, "hipSetDevice(%d): %s", h->device, hipGetErrorString(e));
+    }
+    guard.before = dev;
+  }
+  h->opened = true;
+  return PS_SOFT_OK;
+}
+
+int capturing(ps_soft_t *h, hipStream_t s, bool *out) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (s) SOFT_TRY(h, hipStreamIsCapturing(s, &st));  // the null stream is never captured
+  *out = st == hipStreamCaptureStatusActive;
+  return PS_SOFT_OK;
+}
+
+int grow(ps_soft_t *h, int64_t bytes) {
+  bool cap = false;
+  const int rc = capturing(h, h->stream, &cap);
+  if (rc) return rc;
+  if (cap && bytes > h->work_bytes)
+    return fail(h, PS_SOFT_ESTATE, "the workspace has %lld of %lld bytes and cannot grow while the stream is captured: ps_soft_reserve, or the call itself, before",
+                (long long)h->work_bytes, (long long)bytes);
+  h->captured = h->captured || cap;
+  if (bytes <= h->work_bytes) return PS_SOFT_OK;
+  SOFT_TRY(h, hipStreamSynchronize(h->stream));
+  if (h->work) {
+    if (h->captured) {
+      try {
+        h->kept.push_back(h->work);
+      } catch (const std::bad_alloc &) {
+        return fail(h, PS_SOFT_ENOMEM, "host memory");
+      }
+    } else {
+      (void)hipFree(h->work);
+    }
+    h->work = nullptr;
+    h->work_bytes = 0;
+  }
+  void *p = nullptr;
+  const hipError_t e = hipMalloc(&p, static_cast<size_t>(bytes));
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(h, e == hipErrorOutOfMemory ? PS_SOFT_ENOMEM : PS_SOFT_EDEVICE, "workspace of %lld bytes: %s", (long long)bytes, hipGetErrorString(e));
+  }
+  h->work = static_cast<char *>(p);
+  h->work_bytes = bytes;
+  return PS_SOFT_OK;
+}
+
+// Offsets into the workspace, taken in order
+struct Arena {
+  int64_t at = 0;
+  int64_t take(int64_t bytes) {
+    const int64_t o = at;
+    at += (bytes + 255) / 256 * 256;
+    return o;
+  }
+};
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+unsigned blocks_for(int64_t n, int64_t per, int64_t most) {
+  return static_cast<unsigned>(std::max<int64_t>(1, std::min(up(n, per), most)));
+}
+
+template <class T>
+bool aligned4(const T *p, int64_t ld) {
+  return (reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T))) == 0 && ld % 4 == 0;
+}
+
+// Sizes and places of one call's intermediate values
+struct Plan {
+  int32_t np, k16, kd;
+  int64_t n, entries, xt, wt;  // rows, entries, tiles of each table
+  bool want_dx, want_dw;
+  int64_t x_stride, w_stride;  // halves per tile
+  int32_t rsplits, csplits;
+  int64_t rper, cper;          // tiles per split
+  int64_t chunk, chunks;
+  int32_t sort_blocks, passes;
+  int64_t key[2], row[2], cb[2], coef, act, total, extra, share, gw, row_part, part, scal, px, pw, m, l, o, rowvec, hist, bins, isum, ysum;
+  int64_t bytes;
+};
+
+// Pieces of the reduced axis: enough that the wavefronts (one per 32 own rows and piece) fill 256 CUs four times over, and no
+// piece shorter than 8 tiles
+int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
+  if (forced > 0) return static_cast<int32_t>(std::min<int64_t>(forced, tiles));
+  const int64_t want = up(2048, own_tiles);
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min({want, tiles / 8, static_cast<int64_t>(256)})));
+}
+
+Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
+  Plan p{};
+  p.np = h->type == PS_SOFT_F32 ? 2 : 1;
+  p.k16 = (h->K + 15) / 16;
+  p.kd = (h->K + 31) / 32;
+  p.n = n;
+  p.entries = entries;
+  p.xt = std::max<int64_t>(1, up(n, kTile));  // no row: the plan of one, of which nothing is launched
+  p.wt = up(h->items, kTile);
+  p.want_dx = dx;
+  p.want_dw = dw;
+  p.x_stride = static_cast<int64_t>(p.np) * kFrag * (p.k16 + (dw ? 2 * p.kd : 0));
+  p.w_stride = static_cast<int64_t>(p.np) * kFrag * (p.k16 + (dx ? 2 * p.kd : 0));
+  p.rsplits = pieces(p.xt, p.wt, h->splits);
+  p.rper = up(p.wt, p.rsplits);
+  p.rsplits = static_cast<int32_t>(up(p.wt, p.rper));
+  p.csplits = 0;
+  p.cper = 1;
+  if (dw) {
+    p.csplits = pieces(p.wt, p.xt, h->splits);
+    p.cper = up(p.xt, p.csplits);
+    p.csplits = static_cast<int32_t>(up(p.xt, p.cper));
+  }
+  // a lane group sums 32 entries, more where 16,384 groups would not cover them
+  p.chunk = 32;
+  while (p.chunk < 1024 && up(entries, p.chunk) > 16384) p.chunk *= 2;
+  p.chunks = up(entries, p.chunk);
+  p.sort_blocks = static_cast<int32_t>(up(entries, kSortTile));
+  p.passes = 0;
+  for (int64_t v = h->items; v > 0; v >>= kBits) ++p.passes;
+  Arena a;
+  for (int q = 0; q < 2; ++q) {
+    p.key[q] = a.take(entries * 4);
+    p.row[q] = a.take(dw ? entries * 4 : 0);
+    p.cb[q] = a.take(dw ? entries * 4 : 0);
+  }
+  p.coef = a.take(entries * 4);
+  p.act = a.take(n * 4);
+  p.total = a.take(n * 4);
+  p.extra = a.take(n * 4);
+  p.share = a.take(n * 4);
+  p.gw = a.take(n * 4);
+  p.row_part = a.take(kRowParts * 4);
+  p.part = a.take(2 * kParts * 4);
+  p.scal = a.take(sizeof(Scal));
+  p.px = a.take(p.xt * p.x_stride * 2);
+  p.pw = a.take(p.wt * p.w_stride * 2);
+  const int64_t rpad = p.rsplits * p.xt * kTile, cpad = p.csplits * p.wt * kTile;
+  p.m = a.take(std::max(rpad, cpad) * 4);
+  p.l = a.take(rpad * 4);
+  p.o = a.take(std::max(dx ? rpad : 0, cpad) * p.kd * 32 * 4);
+  p.rowvec = a.take(dw ? p.xt * 64 * 4 : 0);
+  p.hist = a.take(dw ? static_cast<int64_t>(p.sort_blocks) * kBins * 4 : 0);
+  p.bins = a.take(kBins * 4);
+  p.isum = a.take(dw ? 2 * p.chunks * p.kd * 32 * 4 : 0);
+  p.ysum = a.take(dw && entries ? (h->items + 1) * p.kd * 32 * 4 : 0);
+  p.bytes = a.at;
+  return p;
+}
+
+template <int NP, int KC, int DB>
+void launch_pass(const PassArgs &a, bool col, unsigned own_tiles, unsigned splits, hipStream_t s) {
+  const dim3 grid(own_tiles, splits);
+  if (col) {
+    if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((k_pass<NP, KC, DB, false>), grid, dim3(64), 0, s, a);
+  }
+}
+
+// sums: the pass also sums rows.  512 numbers of two planes leave no registers for all sums: two launches of half of
+// them each, with the scores made twice.
+template <int NP>
+void run_pass(PassArgs a, bool col, bool sums, unsigned own_tiles, unsigned splits, hipStream_t s) {
+  const int k = a.k16;
+  a.d0 = 0;
+  if (!sums) {
+    if (k <= 2) launch_pass<NP, 2, 0>(a, false, own_tiles, splits, s);
+    else if (k <= 4) launch_pass<NP, 4, 0>(a, false, own_tiles, splits, s);
+    else if (k <= 8) launch_pass<NP, 8, 0>(a, false, own_tiles, splits, s);
+    else if (k <= 16) launch_pass<NP, 16, 0>(a, false, own_tiles, splits, s);
+    else launch_pass<NP, 32, 0>(a, false, own_tiles, splits, s);
+    return;
+  }
+  if (k <= 2) launch_pass<NP, 2, 1>(a, col, own_tiles, splits, s);
+  else if (k <= 4) launch_pass<NP, 4, 2>(a, col, own_tiles, splits, s);
+  else if (k <= 8) launch_pass<NP, 8, 4>(a, col, own_tiles, splits, s);
+  else if (k <= 16) launch_pass<NP, 16, 8>(a, col, own_tiles, splits, s);
+  else {
+    for (a.d0 = 0; a.d0 < a.kd; a.d0 += 8) launch_pass<NP, 32, 8>(a, col, own_tiles, splits, s);
+  }
+}
+
+template <class T, int G, int V>
+void run_rows(const RowArgs<T> &a, bool dx, bool few, hipStream_t s) {
+  const int64_t rows = a.rowvec ? up(a.n, kTile) * kTile : a.n;
+  if (few) {
+    const dim3 grid(static_cast<unsigned>(rows));
+    if (dx) hipLaunchKernelGGL((k_row_finish<T, G, V, 4, true>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_row_finish<T, G, V, 4, false>), grid, dim3(kThreads), 0, s, a);
+  } else {
+    const dim3 grid(static_cast<unsigned>(up(rows, 4)));
+    if (dx) hipLaunchKernelGGL((k_row_finish<T, G, V, 1, true>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((k_row_finish<T, G, V, 1, false>), grid, dim3(kThreads), 0, s, a);
+  }
+}
+
+template <class T, int G, int V>
+void run_items(const ItemArgs<T> &a, hipStream_t s) {
+  constexpr int per = kThreads / G;
+  if (a.entries > 0)
+    hipLaunchKernelGGL((k_item_lists<T, G, V>), dim3(static_cast<unsigned>(up(a.chunks, per))), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((k_item_finish<T, G, V>), dim3(static_cast<unsigned>(up(a.items, per))), dim3(kThreads), 0, s, a);
+}
+
+// Lanes per row: 4 numbers each, 8 above 256
+template <class F>
+void by_k(int K, F f) {
+  if (K <= 16) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+  else if (K <= 32) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+  else if (K <= 64) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  else if (K <= 128) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+  else if (K <= 256) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+}
+
+// One loss with its gradients; `t` holds the caller's lists
+template <class T, bool Distill>
+int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int64_t ldw, float *loss, float *lse, T *dX,
+              int64_t lddx, T *dW, int64_t lddw) {
+  constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+  const bool dx = dX != nullptr, dw = dW != nullptr;
+  const Plan p = plan(h, t.n, t.entries, dx, dw);
+  int rc = grow(h, p.bytes);
+  if (rc) return rc;
+  char *const base = h->work;
+  auto at_f = [&](int64_t o) { return reinterpret_cast<float *>(base + o); };
+  auto at_i = [&](int64_t o) { return reinterpret_cast<int32_t *>(base + o); };
+  hipStream_t s = h->stream;
+  Scal *scal = reinterpret_cast<Scal *>(base + p.scal);
+  t.items = static_cast<int32_t>(h->items);
+  t.key = at_i(p.key[0]);
+  t.erow = at_i(p.row[0]);
+  t.coef = at_f(p.coef);
+  t.cb = dw ? at_f(p.cb[0]) : nullptr;
+  t.act = at_i(p.act);
+  t.total = at_f(p.total);
+  t.extra = at_f(p.extra);
+  t.share = at_f(p.share);
+  t.gw = at_f(p.gw);
+  t.part = at_f(p.row_part);
+  Table<T> x{X, ldx, t.n, aligned4(X, ldx), t.act}, w{W, ldw, h->items, aligned4(W, ldw), nullptr};
+  _Float16 *px = reinterpret_cast<_Float16 *>(base + p.px), *pw = reinterpret_cast<_Float16 *>(base + p.pw);
+  const float scale = 1.44269504088896340736f / t.tau;
+  if (t.n > 0) {
+    if (t.row_ptr && dw && t.entries > 0)
+      hipLaunchKernelGGL(k_fill_keys, dim3(blocks_for(t.entries, kThreads * 4, 4096)), dim3(kThreads), 0, s, t.key, t.entries, t.items);
+    const unsigned row_blocks = blocks_for(t.n, 4, kRowParts);
+    hipLaunchKernelGGL((k_targets<Distill>), dim3(row_blocks), dim3(kThreads), 0, s, t);
+    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kThreads), 0, s, x, w, h->K, at_f(p.part));
+    const PackSide sx{px, p.x_stride, static_cast<int32_t>(p.xt), dw}, sw{pw, p.w_stride, static_cast<int32_t>(p.wt), dx};
+    hipLaunchKernelGGL((k_pack<T, NP>), dim3(static_cast<unsigned>(p.xt + p.wt)), dim3(kThreads),
+                       static_cast<unsigned>(kTile * (std::min(p.kd, kPackBlocks) * 32 + 1) * 4), s, x, w, sx, sw, h->K, p.k16, p.kd, at_f(p.part),
+                       at_f(p.row_part), static_cast<int32_t>(row_blocks), scal);
+    PassArgs a{};
+    a.own = px;
+    a.own_stride = p.x_stride;
+    a.own_rows = t.n;
+    a.str = pw;
+    a.str_stride = p.w_stride;
+    a.str_rows = h->items;
+    a.k16 = p.k16;
+    a.kd = p.kd;
+    a.scal = scal;
+    a.scale = scale;
+    a.tiles_per_split = p.rper;
+    a.m = at_f(p.m);
+    a.l = at_f(p.l);
+    a.o = at_f(p.o);
+    run_pass<NP>(a, false, dx, static_cast<unsigned>(p.xt), static_cast<unsigned>(p.rsplits), s);
+    RowArgs<T> r{};
+    r.n = t.n;
+    r.entries = t.entries;
+    r.own_pad = p.xt * kTile;
+    r.K = h->K;
+    r.ldo = p.kd * 32;
+    r.k = t.k;
+    r.splits = p.rsplits;
+    r.items = t.items;
+    r.row_ptr = t.row_ptr;
+    r.x = x;
+    r.w = w;
+    r.key = t.key;
+    r.coef = t.coef;
+    r.total = t.total;
+    r.extra = t.extra;
+    r.share = t.share;
+    r.gw = t.gw;
+    r.scal = scal;
+    r.m = a.m;
+    r.l = a.l;
+    r.o = a.o;
+    r.scale = scale;
+    r.inv_tau = 1.f / t.tau;
+    r.gain = t.tau * t.tau;
+    r.loss = loss;
+    r.lse = lse;
+    r.dX = dX;
+    r.lddx = lddx;
+    r.vec_out = dx && aligned4(dX, lddx);
+    r.rowvec = dw ? at_f(p.rowvec) : nullptr;
+    by_k(h->K, [&](auto g, auto v) { run_rows<T, g(), v()>(r, dx, t.n <= 1024, s); });
+    if (dw) {
+      a.own = pw;
+      a.own_stride = p.w_stride;
+      a.own_rows = h->items;
+      a.str = px;
+      a.str_stride = p.x_stride;
+      a.str_rows = t.n;
+      a.rowvec = at_f(p.rowvec);
+      a.tiles_per_split = p.cper;
+      run_pass<NP>(a, true, true, static_cast<unsigned>(p.wt), static_cast<unsigned>(p.csplits), s);
+    }
+  }
+  if (dw) {
+    ItemArgs<T> a{};
+    int from = 0;
+    Entries ent[2] = {{at_i(p.key[0]), at_i(p.row[0]), at_f(p.cb[0])}, {at_i(p.key[1]), at_i(p.row[1]), at_f(p.cb[1])}};
+    if (t.n > 0 && t.entries > 0) {
+      for (int q = 0; q < p.passes; ++q, from ^= 1) {
+        const unsigned blocks = static_cast<unsigned>(p.sort_blocks);
+        hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(kThreads), 0, s, ent[from].key, t.entries, q * kBits, at_i(p.hist), p.sort_blocks);
+        hipLaunchKernelGGL(k_sort_scan, dim3(kBins), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
+        hipLaunchKernelGGL(k_sort_move, dim3(blocks), dim3(kThreads), 0, s, ent[from], ent[from ^ 1], t.entries, q * kBits, at_i(p.hist),
+                           p.sort_blocks, at_i(p.bins));
+      }
+    }
+    a.own_pad = p.wt * kTile;
+    a.entries = t.n > 0 ? t.entries : 0;
+    a.chunk = p.chunk;
+    a.chunks = p.chunks;
+    a.items = t.items;
+    a.K = h->K;
+    a.ldo = p.kd * 32;
+    a.splits = t.n > 0 ? p.csplits : 0;
+    a.kd = p.kd;
+    a.x = x;
+    a.ent = ent[from];
+    a.part = at_f(p.isum);
+    a.ysum = at_f(p.ysum);
+    a.scal = scal;
+    a.m = at_f(p.m);
+    a.o = at_f(p.o);
+    a.dW = dW;
+    a.lddw = lddw;
+    a.vec_out = aligned4(dW, lddw);
+    by_k(h->K, [&](auto g, auto v) { run_items<T, g(), v()>(a, s); });
+  }
+  SOFT_TRY(h, hipGetLastError());
+  return PS_SOFT_OK;
+}
+
+// Rows of one launch of the item search: their exclusion bits and pieces' results stay below a gigabyte
+struct TopPlan {
+  int64_t rows, per;
+  int32_t pieces, words;
+  int64_t bits, key, item, bytes;
+};
+TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
+  TopPlan p{};
+  p.words = static_cast<int32_t>(up(h->items, 32));
+  const int64_t rows = std::max<int64_t>(n, 1);
+  p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min({up(512, rows), up(h->items, kThreads), static_cast<int64_t>(256)})));
+  if (h->splits > 0) p.pieces = static_cast<int32_t>(std::min<int64_t>(h->splits, h->items));
+  p.per = up(h->items, p.pieces);
+  p.pieces = static_cast<int32_t>(up(h->items, p.per));
+  const int64_t per_row = (exclude ? p.words * 4LL : 0) + static_cast<int64_t>(p.pieces) * k * 12;
+  p.rows = std::min(rows, std::max<int64_t>(1, (1LL << 30) / per_row));
+  Arena a;
+  p.bits = a.take(exclude ? p.rows * p.words * 4 : 0);
+  p.key = a.take(p.rows * p.pieces * k * 8);
+  p.item = a.take(p.rows * p.pieces * k * 4);
+  p.bytes = a.at;
+  return p;
+}
+
+template <class T>
+int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64_t ldw, int32_t k, const int64_t *row_ptr,
+             const int32_t *item, int64_t entries, int32_t *top_item, float *top_score, int64_t ldo) {
+  const TopPlan p = top_plan(h, n, k, row_ptr != nullptr);
+  const int rc = grow(h, p.bytes);
+  if (rc) return rc;
+  TopArgs<T> a{};
+  a.items = static_cast<int32_t>(h->items);
+  a.K = h->K;
+  a.k = k;
+  a.words = p.words;
+  a.x = Table<T>{X, ldx, n, aligned4(X, ldx), nullptr};
+  a.w = Table<T>{W, ldw, h->items, aligned4(W, ldw), nullptr};
+  uint32_t *bits = reinterpret_cast<uint32_t *>(h->work + p.bits);
+  a.excluded = row_ptr ? bits : nullptr;
+  a.per_piece = p.per;
+  a.pieces = p.pieces;
+  a.key = reinterpret_cast<uint64_t *>(h->work + p.key);
+  a.item = reinterpret_cast<int32_t *>(h->work + p.item);
+  a.out_item = top_item;
+  a.out_score = top_score;
+  a.ldo = ldo;
+  for (a.row0 = 0; a.row0 < n; a.row0 += p.rows) {
+    a.n = std::min(p.rows, n - a.row0);
+    if (row_ptr) {
+      hipLaunchKernelGGL(k_clear, dim3(blocks_for(a.n * p.words, kThreads * 4, 8192)), dim3(kThreads), 0, h->stream, bits, a.n * p.words);
+      hipLaunchKernelGGL(k_exclude, dim3(static_cast<unsigned>(up(a.n, 4))), dim3(kThreads), 0, h->stream, row_ptr, item, entries, a.row0,
+                         a.n, a.items, p.words, bits);
+    }
+    hipLaunchKernelGGL((k_top_scan<T>), dim3(static_cast<unsigned>(a.n), static_cast<unsigned>(p.pieces)), dim3(kThreads), 0, h->stream, a);
+    hipLaunchKernelGGL((k_top_join<T>), dim3(static_cast<unsigned>(a.n)), dim3(kThreads), 0, h->stream, a);
+  }
+  SOFT_TRY(h, hipGetLastError());
+  return PS_SOFT_OK;
+}
+
+constexpr int64_t kMaxRows = (1LL << 31) - 65;
+
+int check_tables(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw) {
+  if (n < 0 || n > kMaxRows) return fail(h, PS_SOFT_EINVAL, "rows must be in [0, 2^31 - 65], not %lld", (long long)n);
+  if ((n > 0 && !X) || !W) return fail(h, PS_SOFT_EINVAL, "null table");
+  if (ldx < h->K || ldw < h->K) return fail(h, PS_SOFT_EINVAL, "row strides must be at least K = %d", h->K);
+  return PS_SOFT_OK;
+}
+
+int check_outputs(ps_soft_t *h, const void *dX, int64_t lddx, const void *dW, int64_t lddw, int64_t entries) {
+  if ((dX && lddx < h->K) || (dW && lddw < h->K)) return fail(h, PS_SOFT_EINVAL, "gradients' row strides must be at least K = %d", h->K);
+  if (entries < 0 || entries > kMaxRows) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
+  return PS_SOFT_OK;
+}
+
+template <bool Distill>
+int any_loss(ps_soft_t *h, const Targets &t, const void *X, int64_t ldx, const void *W, int64_t ldw, float *loss, float *lse, void *dX,
+             int64_t lddx, void *dW, int64_t lddw) {
+  DeviceGuard guard;
+  const int rc = open(h, guard);
+  if (rc) return rc;
+  switch (h->type) {
+    case PS_SOFT_F32:
+      return soft_loss<float, Distill>(h, t, static_cast<const float *>(X), ldx, static_cast<const float *>(W), ldw, loss, lse,
+                                       static_cast<float *>(dX), lddx, static_cast<float *>(dW), lddw);
+    case PS_SOFT_BF16:
+      return soft_loss<bf16_t, Distill>(h, t, static_cast<const bf16_t *>(X), ldx, static_cast<const bf16_t *>(W), ldw, loss, lse,
+                                        static_cast<bf16_t *>(dX), lddx, static_cast<bf16_t *>(dW), lddw);
+    default:
+      return soft_loss<f16_t, Distill>(h, t, static_cast<const f16_t *>(X), ldx, static_cast<const f16_t *>(W), ldw, loss, lse,
+                                       static_cast<f16_t *>(dX), lddx, static_cast<f16_t *>(dW), lddw);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int ps_soft_create(int64_t items, int32_t K, int32_t type, ps_soft_t **out) {
+  if (!out) return PS_SOFT_EINVAL;
+  *out = nullptr;
+  if (items < 1 || items > kMaxRows || K < 1 || K > kMaxK || type < PS_SOFT_F32 || type > PS_SOFT_F16) return PS_SOFT_EINVAL;
+  ps_soft_t *h = new (std::nothrow) ps_soft_t();
+  if (!h) return PS_SOFT_ENOMEM;
+  h->items = items;
+  h->K = K;
+  h->type = type;
+  *out = h;
+  return PS_SOFT_OK;
+}
+
+int ps_soft_set_option(ps_soft_t *h, int32_t key, int64_t value) {
+  if (!h) return PS_SOFT_EINVAL;
+  switch (key) {
+    case PS_SOFT_OPT_DEVICE:
+      if (value < -1 || value > 4095) return fail(h, PS_SOFT_EINVAL, "device ordinal must be in [-1, 4095]");
+      if (h->opened) return fail(h, PS_SOFT_ESTATE, "the device is already in use");
+      h->device = static_cast<int>(value);
+      return PS_SOFT_OK;
+    case PS_SOFT_OPT_SPLITS:
+      if (value < 0 || value > 1024) return fail(h, PS_SOFT_EINVAL, "pieces must be in [0, 1024]");
+      h->splits = static_cast<int32_t>(value);
+      return PS_SOFT_OK;
+    default:
+      return fail(h, PS_SOFT_EINVAL, "unknown option key %d", key);
+  }
+}
+
+int ps_soft_set_stream(ps_soft_t *h, void *hip_stream) {
+  if (!h) return PS_SOFT_EINVAL;
+  hipStream_t to = static_cast<hipStream_t>(hip_stream);
+  if (h->stream == to || !h->opened) {
+    h->stream = to;
+    return PS_SOFT_OK;
+  }
+  DeviceGuard guard;
+  int rc = open(h, guard);
+  if (rc) return rc;
+  bool from_cap = false, to_cap = false;
+  if ((rc = capturing(h, h->stream, &from_cap)) || (rc = capturing(h, to, &to_cap))) return rc;
+  if (!from_cap && !to_cap) {
+    if (!h->moved) SOFT_TRY(h, hipEventCreateWithFlags(&h->moved, hipEventDisableTiming));
+    SOFT_TRY(h, hipEventRecord(h->moved, h->stream));
+    SOFT_TRY(h, hipStreamWaitEvent(to, h->moved, 0));
+  }
+  h->stream = to;
+  return PS_SOFT_OK;
+}
+
+int ps_soft_reserve(ps_soft_t *h, int64_t n, int64_t entries, int32_t top) {
+  if (!h) return PS_SOFT_EINVAL;
+  if (n < 0 || n > kMaxRows || entries < 0 || entries > kMaxRows || top < 0 || top > kMaxTop)
+    return fail(h, PS_SOFT_EINVAL, "rows and entries must be in [0, 2^31 - 65], top in [0, %d]", kMaxTop);
+  DeviceGuard guard;
+  const int rc = open(h, guard);
+  if (rc) return rc;
+  int64_t bytes = plan(h, n, entries, true, true).bytes;
+  if (top > 0) bytes = std::max(bytes, top_plan(h, n, top, true).bytes);
+  return grow(h, bytes);
+}
+
+int ps_soft_xent(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw, const int64_t *row_ptr,
+                 const int32_t *item, const float *value, int64_t entries, const float *weight, float *loss, float *lse, void *dX,
+                 int64_t lddx, void *dW, int64_t lddw) {
+  if (!h) return PS_SOFT_EINVAL;
+  int rc = check_tables(h, n, X, ldx, W, ldw);
+  if (rc || (rc = check_outputs(h, dX, lddx, dW, lddw, entries))) return rc;
+  if (!row_ptr && entries != n) return fail(h, PS_SOFT_EINVAL, "one target per row takes entries = n");
+  if (entries > 0 && !item) return fail(h, PS_SOFT_EINVAL, "null item list");
+  Targets t{};
+  t.n = n;
+  t.entries = entries;
+  t.k = 1;
+  t.row_ptr = row_ptr;
+  t.item = item;
+  t.value = value;
+  t.tau = 1.f;
+  t.weight = weight;
+  return any_loss<false>(h, t, X, ldx, W, ldw, loss, lse, dX, lddx, dW, lddw);
+}
+
+int ps_soft_distill(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw, int32_t k, const int32_t *item,
+                    const float *score, int64_t ldt, float tau, const float *tlse, const float *weight, float *loss, float *lse,
+                    void *dX, int64_t lddx, void *dW, int64_t lddw) {
+  if (!h) return PS_SOFT_EINVAL;
+  int rc = check_tables(h, n, X, ldx, W, ldw);
+  if (rc) return rc;
+  if (k < 1 || ldt < k) return fail(h, PS_SOFT_EINVAL, "teacher's lists: k = %d, stride %lld", k, (long long)ldt);
+  if (!(tau > 0) || !std::isfinite(tau)) return fail(h, PS_SOFT_EINVAL, "tau must be positive and finite");
+  if (n > 0 && (!item || !score)) return fail(h, PS_SOFT_EINVAL, "null teacher's lists");
+  if ((rc = check_outputs(h, dX, lddx, dW, lddw, n > kMaxRows / k ? kMaxRows + 1 : n * k))) return rc;
+  Targets t{};
+  t.n = n;
+  t.entries = n * k;
+  t.k = k;
+  t.item = item;
+  t.score = score;
+  t.tlse = tlse;
+  t.ldt = ldt;
+  t.tau = tau;
+  t.weight = weight;
+  return any_loss<true>(h, t, X, ldx, W, ldw, loss, lse, dX, lddx, dW, lddw);
+}
+
+int ps_soft_top(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw, int32_t k, const int64_t *row_ptr,
+                const int32_t *item, int64_t entries, int32_t *top_item, float *top_score, int64_t ldo) {
+  if (!h) return PS_SOFT_EINVAL;
+  int rc = check_tables(h, n, X, ldx, W, ldw);
+  if (rc) return rc;
+  if (k < 1 || k > kMaxTop || ldo < k) return fail(h, PS_SOFT_EINVAL, "k must be in [1, %d] and the outputs' stride at least k", kMaxTop);
+  if (entries < 0 || entries > kMaxRows) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
+  if (row_ptr && entries > 0 && !item) return fail(h, PS_SOFT_EINVAL, "null item list");
+  if (n > 0 && (!top_item || !top_score)) return fail(h, PS_SOFT_EINVAL, "null outputs");
+  if (n == 0) return PS_SOFT_OK;
+  DeviceGuard guard;
+  if ((rc = open(h, guard))) return rc;
+  switch (h->type) {
+    case PS_SOFT_F32:
+      return soft_top<float>(h, n, static_cast<const float *>(X), ldx, static_cast<const float *>(W), ldw, k, row_ptr, item, entries,
+                             top_item, top_score, ldo);
+    case PS_SOFT_BF16:
+      return soft_top<bf16_t>(h, n, static_cast<const bf16_t *>(X), ldx, static_cast<const bf16_t *>(W), ldw, k, row_ptr, item, entries,
+                              top_item, top_score, ldo);
+    default:
+      return soft_top<f16_t>(h, n, static_cast<const f16_t *>(X), ldx, static_cast<const f16_t *>(W), ldw, k, row_ptr, item, entries,
+                             top_item, top_score, ldo);
+  }
+}
+
+const char *ps_soft_last_error(const ps_soft_t *h) {
+  return h ? h->err.c_str() : "";
+}
+
+void ps_soft_destroy(ps_soft_t *h) {
+  if (!h) return;
+  if (h->opened) {
+    DeviceGuard guard;
+    int dev = 0;
+    if (hipGetDevice(&dev) == hipSuccess && dev != h->device && hipSetDevice(h->device) == hipSuccess) guard.before = dev;
+    (void)hipStreamSynchronize(h->stream);
+    if (h->work) (void)hipFree(h->work);
+    for (void *p : h->kept) (void)hipFree(p);
+    if (h->moved) (void)hipEventDestroy(h->moved);
+    (void)hipGetLastError();
+  }
+  delete h;
+}
+
+}  // extern "C"
