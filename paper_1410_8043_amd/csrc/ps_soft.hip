@@ -380,9 +380,10 @@ __global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackS
 struct PassArgs {
   const _Float16 *own, *str;
   int64_t own_stride, str_stride;  // halves per tile
-  int64_t own_rows, str_rows;
-  int32_t k16, kd, d0;             // chunks of 16 numbers, blocks of 32, the first block summed here
-  const float *rowvec;             // COL: per tile of 32 stream rows, 32 first values and 32 shares
+  int64_t own_tiles, str_rows;
+  int32_t d0;                      // the first block of 32 numbers summed here
+  int32_t splits, buffers;         // pieces of the stream; tiles in LDS
+  const float *rowvec;             // COL: per tile of 32 stream rows, 32 times minus the log2-sum-exp, and 32 shares
   const Scal *scal;
   float scale;                     // log2(e) / tau
   int64_t tiles_per_split;
@@ -391,17 +392,63 @@ struct PassArgs {
 
 __device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-// Rows over items (COL = false) or items over rows (COL = true).  A wavefront owns 32 rows.
+constexpr int kLds = 160 * 1024;
+constexpr int kWaves = 4;  // wavefronts of a pass's workgroup: 128 own rows
+
+// Fragments of one tile that a pass stages: k16 NP for the scores, then 2 nb NP turned ones
+struct Stage {
+  int scores, turned, halves;  // halves: with the row values of a pass over rows
+};
+__host__ __device__ constexpr Stage stage_of(int np, int k16, int nb, bool col) {
+  Stage s{};
+  s.scores = k16 * np;
+  s.turned = nb * np;  // of each half of the tile's rows
+  s.halves = (s.scores + 2 * s.turned) * kFrag + (col ? 128 : 0);
+  return s;
+}
+
+// Wavefronts per SIMD that the registers are cut for
+constexpr int waves_per_simd(int np, int kc, int db) {
+  const int need = 4 * kc * np + 16 * db + 100;  // own rows, sums, and a tile's scores, weights and fragments
+  return need <= 168 ? 3 : need <= 264 ? 2 : 1;
+}
+
+// Rows over items (COL = false) or items over rows (COL = true).  A wavefront owns 32 rows; the stream's tiles go
+// through LDS, shared by the workgroup, the next one loaded while one is used.
 // Score instruction: stream rows x own rows, so a lane holds one own row (l%32) and 16 stream rows
 // 8(r/4) + 4h + r%4 of each tile.
 template <int NP, int KC, int DB, bool COL>
-__global__ __launch_bounds__(64) void k_pass(PassArgs a) {
-  const int lane = threadIdx.x, half = lane >> 5;
-  const int64_t own_tile = blockIdx.x, own_pad = static_cast<int64_t>(gridDim.x) * kTile;
-  const int64_t split = blockIdx.y;
+__global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
+  constexpr Stage sg = stage_of(NP, KC, DB, COL);
+  constexpr int KD = KC / 2;
+  extern __shared__ _Float16 buf[];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.x % a.splits;
+  const int64_t own_tile = static_cast<int64_t>(blockIdx.x / a.splits) * kWaves + wave;
   const int64_t tiles = (a.str_rows + kTile - 1) / kTile;
   const int64_t t0 = split * a.tiles_per_split, t1 = min(t0 + a.tiles_per_split, tiles);
   const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
+  const bool live = own_tile < a.own_tiles;  // the last workgroup's wavefronts behind the last row only help loading
+  auto fetch = [&](int64_t t, int at) {
+    const _Float16 *src = a.str + t * a.str_stride;
+    _Float16 *to = buf + at * sg.halves;
+#pragma unroll
+    for (int f0 = 0; f0 < sg.scores + 2 * sg.turned; f0 += kWaves) {
+      const int f = f0 + wave;
+      if ((sg.scores + 2 * sg.turned) % kWaves != 0 && f >= sg.scores + 2 * sg.turned) break;
+      int from = f;
+      if (DB > 0 && DB < KD && f >= sg.scores) {
+        const int g = f - sg.scores, q = g >= sg.turned;
+        from = sg.scores + (q * KD + a.d0) * NP + g - q * sg.turned;
+      }
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src + from * kFrag + lane * 8)),
+                                       (__attribute__((address_space(3))) uint32_t *)(to + f * kFrag), 16, 0, 0);
+    }
+    if (COL && wave == 0)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(a.rowvec + t * 64 + lane)),
+                                       (__attribute__((address_space(3))) uint32_t *)(to + sg.halves - 128), 4, 0, 0);
+  };
   h8 q[KC][NP];
   const _Float16 *own = a.own + own_tile * a.own_stride;
 #pragma unroll
@@ -409,81 +456,101 @@ __global__ __launch_bounds__(64) void k_pass(PassArgs a) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       q[c][p] = h8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (c < a.k16) q[c][p] = *reinterpret_cast<const h8 *>(own + (c * NP + p) * kFrag + lane * 8);
+      if (live) q[c][p] = *reinterpret_cast<const h8 *>(own + (c * NP + p) * kFrag + lane * 8);
     }
   f32x16 o[DB > 0 ? DB : 1];
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-  float ref = kNone, sum = 0.f;
+  float ref = kNone, sum = 0.f, lost = 0.f;
+  int at = 0;
+  if (a.buffers == 2) fetch(t0, 0);
   for (int64_t t = t0; t < t1; ++t) {
-    const _Float16 *st = a.str + t * a.str_stride;
+    if (a.buffers == 1) {
+      __syncthreads();
+      fetch(t, 0);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (a.buffers == 2 && t + 1 < t1) fetch(t + 1, at ^ 1);
+    const _Float16 *st = buf + at * sg.halves;
+    if (a.buffers == 2) at ^= 1;
     f32x16 s;
-    float share[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const h8 h = *reinterpret_cast<const h8 *>(st + (c * NP) * kFrag + lane * 8);
+      s = mfma(h, q[c][0], s);
+      if constexpr (NP == 2) {
+        const h8 l = *reinterpret_cast<const h8 *>(st + (c * NP + 1) * kFrag + lane * 8);
+        s = mfma(h, q[c][1], s);
+        s = mfma(l, q[c][0], s);
+      }
+    }
+    // log2 weights: the score's, less the row's log-sum-exp where it is known.  That is subtracted here: as the
+    // matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
+    float p[16], share[16];
     if constexpr (COL) {
-      const float *rv = a.rowvec + t * 64;
+      const float *rv = reinterpret_cast<const float *>(st + sg.halves - 128);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const f32x4 v = *reinterpret_cast<const f32x4 *>(rv + g * 8 + half * 4);
         const f32x4 u = *reinterpret_cast<const f32x4 *>(rv + 32 + g * 8 + half * 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[g * 4 + i] = v[i];
+          p[g * 4 + i] = fmaf(s[g * 4 + i], sc, v[i]);
           share[g * 4 + i] = u[i];
         }
       }
     } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.f;
-    }
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      if (c < a.k16) {
-        const h8 h = *reinterpret_cast<const h8 *>(st + (c * NP) * kFrag + lane * 8);
-        s = mfma(h, q[c][0], s);
-        if constexpr (NP == 2) {
-          const h8 l = *reinterpret_cast<const h8 *>(st + (c * NP + 1) * kFrag + lane * 8);
-          s = mfma(h, q[c][1], s);
-          s = mfma(l, q[c][0], s);
-        }
-      }
-    }
-    if constexpr (!COL) {
+      for (int r = 0; r < 16; ++r) p[r] = s[r] * sc;
       if ((t + 1) * kTile > a.str_rows) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.str_rows) s[r] = -__builtin_inff();
+          if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.str_rows) p[r] = -__builtin_inff();
       }
     }
-    float top = s[0];
+    float top = p[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-    top = fmaxf(top, __shfl_xor(top, 32)) * sc;
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
+    top = fmaxf(top, __shfl_xor(top, 32));
     if (__any(top > ref + kLag)) {
       const float to = top > ref + kLag ? top : ref;
       const float down = __builtin_amdgcn_exp2f(ref - to);
       ref = to;
       sum *= down;
+      lost *= down;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[b][r] *= down;
     }
-    float p[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc, kShift - ref));
+      p[r] = __builtin_amdgcn_exp2f(p[r] + (kShift - ref));
       if constexpr (COL) {
         p[r] *= share[r];
         // the product and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
         // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
         asm("" : "+v"(p[r]));
       }
-      if constexpr (!COL) sum += p[r];
+    }
+    if constexpr (!COL) {
+      // the tile's sum first, and what each addition loses kept: one by one, thousands of small weights were rounded
+      // away against the sum (6e-6 of it over 17,770 items)
+      float w[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) w[r] = p[r] + p[r + 8];
+      const float add = (((w[0] + w[4]) + (w[1] + w[5])) + ((w[2] + w[6]) + (w[3] + w[7]))) - lost;
+      const float now = sum + add;
+      lost = (now - sum) - add;
+      sum = now;
     }
     if constexpr (DB > 0) {
-      const _Float16 *turned = st + a.k16 * NP * kFrag;
+      const _Float16 *turned = st + sg.scores * kFrag + lane * 8;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         h8 ph, pl;
@@ -494,18 +561,17 @@ __global__ __launch_bounds__(64) void k_pass(PassArgs a) {
         }
 #pragma unroll
         for (int b = 0; b < DB; ++b) {
-          if (a.d0 + b < a.kd) {
-            const _Float16 *f = turned + ((k * a.kd + a.d0 + b) * NP) * kFrag + lane * 8;
-            const h8 h = *reinterpret_cast<const h8 *>(f);
-            o[b] = mfma(h, ph, o[b]);
-            o[b] = mfma(h, pl, o[b]);
-            if constexpr (NP == 2) o[b] = mfma(*reinterpret_cast<const h8 *>(f + kFrag), ph, o[b]);
-          }
+          const _Float16 *f = turned + (k * sg.turned + b * NP) * kFrag;
+          const h8 h = *reinterpret_cast<const h8 *>(f);
+          o[b] = mfma(h, ph, o[b]);
+          o[b] = mfma(h, pl, o[b]);
+          if constexpr (NP == 2) o[b] = mfma(*reinterpret_cast<const h8 *>(f + kFrag), ph, o[b]);
         }
       }
     }
   }
-  const int64_t row = split * own_pad + own_tile * kTile + (lane & 31);
+  if (!live) return;
+  const int64_t row = split * (a.own_tiles * kTile) + own_tile * kTile + (lane & 31);
   if (a.d0 == 0) {
     sum += __shfl_xor(sum, 32);
     if (half == 0) {
@@ -514,14 +580,12 @@ __global__ __launch_bounds__(64) void k_pass(PassArgs a) {
     }
   }
   if constexpr (DB > 0) {
-    float *to = a.o + row * (a.kd * 32) + a.d0 * 32 + half * 4;
+    float *to = a.o + row * (KD * 32) + a.d0 * 32 + half * 4;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
-      if (a.d0 + b < a.kd) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<f32x4 *>(to + b * 32 + g * 8) = f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
-      }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4 *>(to + b * 32 + g * 8) = f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
   }
 }
 
@@ -543,7 +607,7 @@ struct RowArgs {
   const float *coef, *total, *extra, *share, *gw;
   const Scal *scal;
   const float *m, *l, *o;
-  float scale, inv_tau, gain;
+  float inv_tau, gain;
   float *loss, *lse;
   T *dX;
   int64_t lddx;
@@ -653,8 +717,7 @@ __global__ __launch_bounds__(kThreads) void k_row_finish(RowArgs<T> a) {
     if (a.loss) a.loss[i] = a.gain * (loss + a.extra[i]);
     if (a.lse) a.lse[i] = lse;
     if (a.rowvec) {
-      const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
-      a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 / sc : -__builtin_inff();
+      a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 : -__builtin_inff();
       a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.share[i] / a.scal->amax : 0.f;
     }
   }
@@ -1215,19 +1278,29 @@ struct Plan {
   int64_t bytes;
 };
 
-// Pieces of the reduced axis: enough that the wavefronts (one per 32 own rows and piece) fill 256 CUs four times over, and no
-// piece shorter than 8 tiles
+// Chunks of 16 numbers that rows are padded to: the passes are built for these
+int32_t padded_chunks(int32_t K) {
+  for (int32_t c : {2, 4, 6, 8, 12, 16})
+    if (K <= 16 * c) return c;
+  return 32;
+}
+
+// Pieces of the reduced axis, each its own workgroups: enough of them for 256 CUs three times over, and a multiple
+// of 8 where the axis is long: workgroup b runs on XCD b mod 8 and takes piece b mod pieces, so the
+// part of the stream that an XCD's L2 sees is an eighth of it.  No piece shorter than 8 tiles.
 int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   if (forced > 0) return static_cast<int32_t>(std::min<int64_t>(forced, tiles));
-  const int64_t want = up(2048, own_tiles);
-  return static_cast<int32_t>(std::max<int64_t>(1, std::min({want, tiles / 8, static_cast<int64_t>(256)})));
+  const int64_t most = std::max<int64_t>(1, tiles / 8);
+  int64_t want = up(768, up(own_tiles, kWaves));
+  if (most >= 8) want = up(want, 8) * 8;
+  return static_cast<int32_t>(std::min({want, most, static_cast<int64_t>(256)}));
 }
 
 Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   Plan p{};
   p.np = h->type == PS_SOFT_F32 ? 2 : 1;
-  p.k16 = (h->K + 15) / 16;
-  p.kd = (h->K + 31) / 32;
+  p.k16 = padded_chunks(h->K);
+  p.kd = p.k16 / 2;
   p.n = n;
   p.entries = entries;
   p.xt = std::max<int64_t>(1, up(n, kTile));  // no row: the plan of one, of which nothing is launched
@@ -1284,35 +1357,38 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
 }
 
 template <int NP, int KC, int DB>
-void launch_pass(const PassArgs &a, bool col, unsigned own_tiles, unsigned splits, hipStream_t s) {
-  const dim3 grid(own_tiles, splits);
+void launch_pass(PassArgs a, bool col, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(up(a.own_tiles, kWaves) * a.splits));
+  const int bytes = stage_of(NP, KC, DB, col).halves * 2;
+  a.buffers = 2 * bytes <= kLds ? 2 : 1;
+  const unsigned lds = static_cast<unsigned>(a.buffers * bytes);
   if (col) {
-    if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64), 0, s, a);
+    if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64 * kWaves), lds, s, a);
   } else {
-    hipLaunchKernelGGL((k_pass<NP, KC, DB, false>), grid, dim3(64), 0, s, a);
+    hipLaunchKernelGGL((k_pass<NP, KC, DB, false>), grid, dim3(64 * kWaves), lds, s, a);
   }
 }
 
 // sums: the pass also sums rows.  512 numbers of two planes leave no registers for all sums: two launches of half of
 // them each, with the scores made twice.
-template <int NP>
-void run_pass(PassArgs a, bool col, bool sums, unsigned own_tiles, unsigned splits, hipStream_t s) {
-  const int k = a.k16;
+template <int NP, int KC>
+void run_pass_of(PassArgs a, bool col, bool sums, hipStream_t s) {
+  constexpr int KD = KC / 2, DB = std::min(KD, 8);
   a.d0 = 0;
-  if (!sums) {
-    if (k <= 2) launch_pass<NP, 2, 0>(a, false, own_tiles, splits, s);
-    else if (k <= 4) launch_pass<NP, 4, 0>(a, false, own_tiles, splits, s);
-    else if (k <= 8) launch_pass<NP, 8, 0>(a, false, own_tiles, splits, s);
-    else if (k <= 16) launch_pass<NP, 16, 0>(a, false, own_tiles, splits, s);
-    else launch_pass<NP, 32, 0>(a, false, own_tiles, splits, s);
-    return;
-  }
-  if (k <= 2) launch_pass<NP, 2, 1>(a, col, own_tiles, splits, s);
-  else if (k <= 4) launch_pass<NP, 4, 2>(a, col, own_tiles, splits, s);
-  else if (k <= 8) launch_pass<NP, 8, 4>(a, col, own_tiles, splits, s);
-  else if (k <= 16) launch_pass<NP, 16, 8>(a, col, own_tiles, splits, s);
-  else {
-    for (a.d0 = 0; a.d0 < a.kd; a.d0 += 8) launch_pass<NP, 32, 8>(a, col, own_tiles, splits, s);
+  if (!sums) launch_pass<NP, KC, 0>(a, false, s);
+  else
+    for (; a.d0 < KD; a.d0 += DB) launch_pass<NP, KC, DB>(a, col, s);
+}
+template <int NP>
+void run_pass(const PassArgs &a, int k16, bool col, bool sums, hipStream_t s) {
+  switch (k16) {
+    case 2: return run_pass_of<NP, 2>(a, col, sums, s);
+    case 4: return run_pass_of<NP, 4>(a, col, sums, s);
+    case 6: return run_pass_of<NP, 6>(a, col, sums, s);
+    case 8: return run_pass_of<NP, 8>(a, col, sums, s);
+    case 12: return run_pass_of<NP, 12>(a, col, sums, s);
+    case 16: return run_pass_of<NP, 16>(a, col, sums, s);
+    default: return run_pass_of<NP, 32>(a, col, sums, s);
   }
 }
 
@@ -1390,19 +1466,18 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     PassArgs a{};
     a.own = px;
     a.own_stride = p.x_stride;
-    a.own_rows = t.n;
+    a.own_tiles = p.xt;
+    a.splits = p.rsplits;
     a.str = pw;
     a.str_stride = p.w_stride;
     a.str_rows = h->items;
-    a.k16 = p.k16;
-    a.kd = p.kd;
     a.scal = scal;
     a.scale = scale;
     a.tiles_per_split = p.rper;
     a.m = at_f(p.m);
     a.l = at_f(p.l);
     a.o = at_f(p.o);
-    run_pass<NP>(a, false, dx, static_cast<unsigned>(p.xt), static_cast<unsigned>(p.rsplits), s);
+    run_pass<NP>(a, p.k16, false, dx, s);
     RowArgs<T> r{};
     r.n = t.n;
     r.entries = t.entries;
@@ -1425,7 +1500,6 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     r.m = a.m;
     r.l = a.l;
     r.o = a.o;
-    r.scale = scale;
     r.inv_tau = 1.f / t.tau;
     r.gain = t.tau * t.tau;
     r.loss = loss;
@@ -1438,13 +1512,14 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     if (dw) {
       a.own = pw;
       a.own_stride = p.w_stride;
-      a.own_rows = h->items;
+      a.own_tiles = p.wt;
+      a.splits = p.csplits;
       a.str = px;
       a.str_stride = p.x_stride;
       a.str_rows = t.n;
       a.rowvec = at_f(p.rowvec);
       a.tiles_per_split = p.cper;
-      run_pass<NP>(a, true, true, static_cast<unsigned>(p.wt), static_cast<unsigned>(p.csplits), s);
+      run_pass<NP>(a, p.k16, true, true, s);
     }
   }
   if (dw) {
