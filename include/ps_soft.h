@@ -101,7 +101,7 @@ int ps_soft_reserve(ps_soft_t *h, int64_t n, int64_t entries, int32_t top);
  *   loss [n], lse [n]: fp32; NULL: not wanted.
  *   dX (n x K, stride lddx), dW (items x K, stride lddw): of the handle's type, sums in fp32
  *     rounded once; NULL: not wanted.  Written, not added to; the space between rows is left.
- * n = 0 is allowed (dW is then zero).
+ * 0 <= n <= 2^26 (n = 0: dW is zero); entries <= 2^31 - 65.
  */
 int ps_soft_xent(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw,
                  const int64_t *row_ptr, const int32_t *item, const float *value, int64_t entries,

@@ -43,7 +43,7 @@ constexpr int kFrag = 512;      // halves of one fragment: 64 lanes x 8
 constexpr int kThreads = 256;
 constexpr int kPackBlocks = 8;  // blocks of 32 numbers that packing holds in LDS at once
 constexpr int kParts = 256;     // workgroups, and partial maxima, of each table's scan
-constexpr int kRowParts = 1024; // most workgroups, and partial maxima, of the row scan
+constexpr int kRowParts = 4096; // most workgroups, and partial maxima, of the row scan
 constexpr float kNone = -1e30f; // reference before the first tile: finite, so that 2^(-inf - kNone) is 0
 // p' = 2^(score - reference + kShift), and the reference follows the maximum when it is exceeded by more than
 // kLag: p' stays below 2^15, and a weight of 2^-17 of the largest keeps 22 bits
@@ -123,11 +123,12 @@ __device__ inline float block_max(float v, float *sh) {  // kThreads threads; sh
 }
 
 // ------------------------------------------------------------------ targets
-// What a call's rows and targets become before the passes.  Entry e of the lists: key (its item, or
-// `items` where it is none), coef (v or q), cb (its share weight tau coef of the gradients), erow (its row).
+// A call's rows and targets before the passes.  Where dW is wanted, each entry of the lists also becomes a record for
+// the pass over rows: key, the tile of 32 items that its item lies in (or `dead`, one behind the last), and a
+// payload of row * 32 + item mod 32 and its share weight tau coef of the gradients.
 struct Targets {
   int64_t n, entries;
-  int32_t items, k;  // k: entries per row without row_ptr
+  int32_t items, k, dead;    // k: entries per row without row_ptr
   const int64_t *row_ptr;
   const int32_t *item;
   const float *value;        // xent
@@ -135,11 +136,11 @@ struct Targets {
   int64_t ldt;
   float tau;
   const float *weight;
-  int32_t *key, *erow;
-  float *coef, *cb;
-  int32_t *act;                          // [n] 0: masked
-  float *total, *extra, *share, *gw;     // [n] sum of coef; sum q log q (NaN: a bad row); gw total; weight tau
-  float *part;                           // [gridDim.x] largest |share|
+  int32_t *key;              // NULL: no dW
+  uint2 *pay;
+  int32_t *act;                             // [n] 0: masked
+  float *total, *extra, *share, *gw, *logz; // [n] sum of coef; sum q log q (NaN: a bad row); gw total; weight tau; the teacher's log-sum-exp
+  float *part;                              // [gridDim.x] largest |gw| sum |coef|
 };
 
 __device__ inline bool row_range(const int64_t *row_ptr, int64_t entries, int32_t k, int64_t i, int64_t &b, int64_t &e) {
@@ -157,12 +158,12 @@ __device__ inline bool row_range(const int64_t *row_ptr, int64_t entries, int32_
   return true;
 }
 
-__global__ __launch_bounds__(kThreads) void k_fill_keys(int32_t *key, int64_t entries, int32_t items) {
+__global__ __launch_bounds__(kThreads) void k_fill_keys(int32_t *key, int64_t entries, int32_t dead) {
   for (int64_t e = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; e < entries; e += static_cast<int64_t>(gridDim.x) * kThreads)
-    key[e] = items;
+    key[e] = dead;
 }
 
-// One wavefront per row.  Bound by the reads of the lists.
+// One wavefront per row.  Bound by the reads of the lists and the writes of the records.
 template <bool Distill>
 __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
   __shared__ float sh[4];
@@ -175,30 +176,24 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
     bool bad = !row_range(a.row_ptr, a.entries, a.k, i, b, e);
     const int64_t src = Distill ? i * a.ldt - b : 0;  // the lists' stride
     const float w = a.weight ? a.weight[i] : 1.f;
-    bool live = false;
-    float top = -inf, den = 1.f;
-    for (int64_t x = b + lane; x < e; x += 64) {
-      const int32_t j = a.item[x + src];
-      if (j >= a.items) bad = true;
-      bool here = j >= 0 && j < a.items;
-      if constexpr (Distill) {
-        const float t = here ? a.score[x + src] : -inf;
-        here = here && !(t == -inf);
-        if (here) top = t != t ? t : fmaxf(top, t / a.tau);
-      }
-      live = live || here;
-    }
-    live = __any(live);
-    bad = __any(bad);
-    const bool act = live && w != 0.f;
     float z = 0.f;  // log of the teacher's sum
     if constexpr (Distill) {
-      if (act) {
+      bool some = false;
+      float top = -inf;
+      for (int64_t x = b + lane; x < e; x += 64) {
+        const int32_t j = a.item[x + src];
+        const float t = j >= 0 && j < a.items ? a.score[x + src] : -inf;
+        if (!(t == -inf)) {
+          some = true;
+          top = t != t ? t : fmaxf(top, t / a.tau);
+        }
+      }
+      if (__any(some)) {
         if (a.tlse) {
           z = a.tlse[i];
         } else {
           top = wave_max(top);
-          den = 0.f;
+          float den = 0.f;
           for (int64_t x = b + lane; x < e; x += 64) {
             const int32_t j = a.item[x + src];
             const float t = j >= 0 && j < a.items ? a.score[x + src] : -inf;
@@ -208,44 +203,47 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
         }
       }
     }
-    float total = 0.f, extra = 0.f;
-    const float gw = act ? w * a.tau : 0.f;
+    bool live = false;
+    float total = 0.f, size = 0.f, extra = 0.f;
+    float gw = w * a.tau;
     for (int64_t x = b + lane; x < e; x += 64) {
       const int32_t j = a.item[x + src];
+      bad = bad || j >= a.items;
+      bool here = j >= 0 && j < a.items;
       float c = 0.f;
-      bool here = act && j >= 0 && j < a.items;
       if (here) {
         if constexpr (Distill) {
           const float t = a.score[x + src];
-          if (t == -inf) {
-            here = false;
-          } else {
-            const float lq = t / a.tau - z;
-            c = expf(lq);
-            extra += c == 0.f ? 0.f : c * lq;
-          }
+          here = !(t == -inf);
+          const float lq = t / a.tau - z;
+          c = here ? expf(lq) : 0.f;
+          extra += c == 0.f ? 0.f : c * lq;
         } else {
           c = a.value ? a.value[x] : 1.f;
         }
       }
-      a.key[x] = here ? j : a.items;
-      a.coef[x] = c;
-      if (a.cb) {
-        a.cb[x] = gw * c;
-        a.erow[x] = static_cast<int32_t>(i);
+      live = live || here;
+      if (a.key) {
+        a.key[x] = here && w != 0.f ? j >> 5 : a.dead;
+        a.pay[x] = make_uint2(static_cast<uint32_t>(i) << 5 | (j & 31), __float_as_uint(gw * c));
       }
       total += c;
+      size += fabsf(c);
     }
+    const bool act = __any(live) && w != 0.f;
+    bad = __any(bad);
+    if (!act) gw = total = size = extra = 0.f;
     total = wave_sum(total);
     extra = wave_sum(extra);
-    const float share = gw * total;
-    most = fmaxf(most, fabsf(share) < inf ? fabsf(share) : 0.f);
+    size = fabsf(gw) * wave_sum(size);
+    most = fmaxf(most, size < inf ? size : 0.f);
     if (lane == 0) {
       a.act[i] = act;
       a.total[i] = total;
       a.extra[i] = bad ? __builtin_nanf("") : extra;
-      a.share[i] = share;
+      a.share[i] = gw * total;
       a.gw[i] = gw;
+      if constexpr (Distill) a.logz[i] = z;
     }
   }
   most = block_max(most, sh);
@@ -295,7 +293,7 @@ __device__ inline int scale_exp(float most) {
 // Scalars that the kernels share
 struct Scal {
   int32_t ex, ew;  // x~ = x 2^ex, w~ = w 2^ew
-  float amax;      // a power of two >= every |share| (1 where all are 0)
+  float amax;      // a power of two >= 2 |gw| sum |coef| of every row (1 where all are 0)
   float pad;
 };
 
@@ -330,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackS
       for (int q = threadIdx.x; q < row_parts; q += kThreads) m = fmaxf(m, row_part[q]);
       __syncthreads();
       m = block_max(m, sh);
-      if (threadIdx.x == 0) scal->amax = m > 0.f ? ldexpf(1.f, 14 - scale_exp(m)) : 1.f;
+      if (threadIdx.x == 0) scal->amax = m > 0.f ? ldexpf(1.f, min(max(15 - scale_exp(m), -100), 126)) : 1.f;
     }
   }
   _Float16 *out = ps.out + at * ps.stride;
@@ -387,12 +385,15 @@ struct PassArgs {
   const Scal *scal;
   float scale;                     // log2(e) / tau
   int64_t tiles_per_split;
+  const int64_t *first;            // COL: where the records of each own tile start ([own tiles + 1], NULL: none)
+  const uint2 *pay;                // sorted by own tile, then row
   float *m, *l, *o;                // [splits][own rows padded]: reference, sum of p', sums [..][32 kd]
 };
 
 __device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 constexpr int kLds = 160 * 1024;
+constexpr int kHalfTile = kTile * 16;  // floats of half a tile's targets
 constexpr int kWaves = 4;  // wavefronts of a pass's workgroup: 128 own rows
 
 // Fragments of one tile that a pass stages: k16 NP for the scores, then 2 nb NP turned ones
@@ -405,6 +406,47 @@ __host__ __device__ constexpr Stage stage_of(int np, int k16, int nb, bool col) 
   s.turned = nb * np;  // of each half of the tile's rows
   s.halves = (s.scores + 2 * s.turned) * kFrag + (col ? 128 : 0);
   return s;
+}
+
+// The sorted target records of one own tile, in windows of 64, one per lane, three windows read ahead
+struct Window {
+  const uint2 *pay;
+  int64_t base, end;
+  uint2 now, next[3];
+  int pos;
+  // a record behind the last: a row above all
+  __device__ uint2 get(int64_t at) const { return at < end ? pay[at] : make_uint2(0xffffffffu, 0u); }
+  __device__ void open(const uint2 *p, int64_t b, int64_t e, int lane) {
+    pay = p;
+    base = b + lane;
+    end = e;
+    pos = 0;
+    now = get(base);
+    for (int q = 0; q < 3; ++q) next[q] = get(base + 64 * (q + 1));
+  }
+  __device__ void step() {
+    base += 64;
+    pos = 0;
+    now = next[0];
+    next[0] = next[1];
+    next[1] = next[2];
+    next[2] = get(base + 192);
+  }
+};
+
+// The first of records [b, e) whose row is at least `row` (rows ascend): all lanes probe at once
+__device__ inline int64_t first_of_row(const uint2 *pay, int64_t b, int64_t e, uint32_t row, int lane) {
+  while (e - b > 0) {
+    const int64_t step = (e - b + 63) / 64;
+    const int64_t at = b + lane * step;
+    const bool below = at < e && (pay[at].x >> 5) < row;
+    const int n = __popcll(__ballot(below));  // lanes 0 .. n-1 are below
+    if (n == 0) return b;
+    const int64_t lo = b + (n - 1) * step + 1;
+    e = min(b + n * step, e);
+    b = lo;
+  }
+  return b;
 }
 
 // Wavefronts per SIMD that the registers are cut for
@@ -463,7 +505,28 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   for (int b = 0; b < DB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-  float ref = kNone, sum = 0.f, lost = 0.f;
+  // Rows of an own tile with targets are the softmax's weights less the targets', which are of size 1 whatever the softmax's
+  // are: the reference stays at -kLag (weights <= 1), and small weights keep 2^-25 of 2^15.  Elsewhere it
+  // follows the largest weight.
+  float ref = kNone, sum = 0.f, lost = 0.f, unit = 0.f;
+  bool targets = false;
+  Window win;
+  float *y = nullptr;
+  if constexpr (COL) {
+    y = reinterpret_cast<float *>(buf + a.buffers * sg.halves) + wave * kHalfTile;
+#pragma unroll
+    for (int r = 0; r < kHalfTile / 64; ++r) y[r * 64 + lane] = 0.f;
+    if (a.first && live) {
+      const int64_t b = first_of_row(a.pay, a.first[own_tile], a.first[own_tile + 1], static_cast<uint32_t>(t0 * kTile), lane);
+      const int64_t e = a.first[own_tile + 1];
+      win.open(a.pay, b, e, lane);
+      targets = __any(win.now.x >> 5 < static_cast<uint64_t>(t1) * kTile);
+    }
+    if (targets) {
+      ref = -kLag;
+      unit = ldexpf(1.f / a.scal->amax, static_cast<int>(kShift + kLag));
+    }
+  }
   int at = 0;
   if (a.buffers == 2) fetch(t0, 0);
   for (int64_t t = t0; t < t1; ++t) {
@@ -513,30 +576,27 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.str_rows) p[r] = -__builtin_inff();
       }
     }
-    float top = p[0];
+    if (!COL || !targets) {
+      float top = p[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (__any(top > ref + kLag)) {
-      const float to = top > ref + kLag ? top : ref;
-      const float down = __builtin_amdgcn_exp2f(ref - to);
-      ref = to;
-      sum *= down;
-      lost *= down;
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > ref + kLag)) {
+        const float to = top > ref + kLag ? top : ref;
+        const float down = __builtin_amdgcn_exp2f(ref - to);
+        ref = to;
+        sum *= down;
+        lost *= down;
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
+        for (int b = 0; b < DB; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] *= down;
+          for (int r = 0; r < 16; ++r) o[b][r] *= down;
+      }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       p[r] = __builtin_amdgcn_exp2f(p[r] + (kShift - ref));
-      if constexpr (COL) {
-        p[r] *= share[r];
-        // the product and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
-        // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
-        asm("" : "+v"(p[r]));
-      }
+      if constexpr (COL) p[r] *= share[r];
     }
     if constexpr (!COL) {
       // the tile's sum first, and what each addition loses kept: one by one, thousands of small weights were rounded
@@ -553,6 +613,45 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       const _Float16 *turned = st + sg.scores * kFrag + lane * 8;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
+        if (COL && targets) {
+          // this half tile's records, through the wavefront's own table of 32 items x 16 rows in LDS, zero between uses.  A
+          // row that lists an item twice adds twice: one wavefront's LDS additions come in the order of its
+          // instructions and, within one, in an order that its addresses alone decide.
+          const uint32_t limit = static_cast<uint32_t>(t * kTile + 16 * k + 16);
+          bool some = false;
+          for (;;) {
+            const bool mine = lane >= win.pos && (win.now.x >> 5) < limit;
+            const int n = __popcll(__ballot(mine));
+            if (n == 0) break;
+            some = true;
+            if (mine) {
+              const uint32_t r = (win.now.x >> 5) & 15, c = win.now.x & 31;
+              atomicAdd(y + c * 16 + (((r >> 2) ^ ((c >> 2) & 3)) << 2) + (r & 3), __uint_as_float(win.now.y) * unit);
+            }
+            win.pos += n;
+            if (win.pos < 64) break;
+            win.step();
+          }
+          if (some) {
+            __builtin_amdgcn_wave_barrier();
+            const int col = lane & 31, turn = (col >> 2) & 3;
+            f32x4 *const y0 = reinterpret_cast<f32x4 *>(y + col * 16 + ((half ^ turn) << 2));
+            f32x4 *const y1 = reinterpret_cast<f32x4 *>(y + col * 16 + (((2 + half) ^ turn) << 2));
+            const f32x4 v0 = *y0, v1 = *y1;
+            __builtin_amdgcn_wave_barrier();
+            *y0 = *y1 = f32x4{0.f, 0.f, 0.f, 0.f};
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              p[8 * k + i] -= v0[i];
+              p[8 * k + 4 + i] -= v1[i];
+            }
+          }
+        }
+        // a weight and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
+        // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) asm("" : "+v"(p[8 * k + i]));
         h8 ph, pl;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -599,15 +698,12 @@ __device__ inline void load_row(f32x4 (&x)[V], const T *row, int g, int K, bool 
 
 template <class T>
 struct RowArgs {
-  int64_t n, entries, own_pad;
-  int32_t K, ldo, k, splits, items;
-  const int64_t *row_ptr;
+  Targets t;
+  int64_t own_pad;
+  int32_t K, ldo, splits;
   Table<T> x, w;
-  const int32_t *key;
-  const float *coef, *total, *extra, *share, *gw;
   const Scal *scal;
   const float *m, *l, *o;
-  float inv_tau, gain;
   float *loss, *lse;
   T *dX;
   int64_t lddx;
@@ -615,24 +711,27 @@ struct RowArgs {
   float *rowvec;  // NULL: no pass over rows follows
 };
 
-// TW wavefronts per row (4: few rows with long lists).  Gathers of the target items' rows bound it.
-template <class T, int G, int V, int TW, bool DX>
-__global__ __launch_bounds__(kThreads) void k_row_finish(RowArgs<T> a) {
-  constexpr int NG = TW * 64 / G;  // groups per row
-  constexpr int RF = 4;            // rows in flight per group
-  __shared__ float part[TW == 4 ? 4 : 1][TW == 4 ? 64 * 4 * V + 1 : 1];
+// TW wavefronts per row (more for few rows).  The targets' part is c_i = sum coef w_j: dX_i needs it, and the loss
+// too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it.
+template <class T, int G, int V, int TW>
+__global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowArgs<T> a) {
+  constexpr int NG = TW * 64 / G;      // groups per row
+  constexpr int RF = V == 1 ? 8 : 4;   // rows in flight per group
+  constexpr int RB = TW == 16 ? 1 : 4 / TW;  // rows per workgroup
+  __shared__ f32x4 part[TW > 1 ? TW : 1][TW > 1 ? 2 * V * G : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = lane & (G - 1);
-  const int grp = (TW == 4 ? wave * (64 / G) : 0) + lane / G;
-  const int64_t i = TW == 4 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
-  const int64_t row_end = (a.n + kTile - 1) / kTile * kTile;
-  if (i >= a.n) {  // rows behind the last, to the end of its tile: no weight in the pass over rows
+  const int grp = (TW > 1 ? wave * (64 / G) : 0) + lane / G;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * RB + (TW == 1 ? wave : 0);
+  const int64_t row_end = (a.t.n + kTile - 1) / kTile * kTile;
+  if (i >= a.t.n) {  // rows behind the last, to the end of its tile: no weight in the pass over rows
     if (a.rowvec && i < row_end && lane == 0 && (TW == 1 || wave == 0)) {
       a.rowvec[(i >> 5) * 64 + (i & 31)] = -__builtin_inff();
       a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = 0.f;
     }
     return;
   }
+  const bool act = a.t.act[i];
   float top = kNone;
   for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.m[s * a.own_pad + i]);
   float den = 0.f;
@@ -640,125 +739,137 @@ __global__ __launch_bounds__(kThreads) void k_row_finish(RowArgs<T> a) {
     den += a.l[s * a.own_pad + i] * __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
   const float lse2 = top - kShift + log2f(den);
   const float lse = lse2 * 0.69314718055994530942f;
-  const bool act = !a.x.act || a.x.act[i];
-  f32x4 x[V], acc[V];
+  f32x4 acc[V], o[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (act) load_row<T, G, V>(x, a.x.p + i * a.x.ld, g, a.K, a.x.vec);
-  float loss = 0.f;
-  int64_t b, e;
-  row_range(a.row_ptr, a.entries, a.k, i, b, e);
+  for (int v = 0; v < V; ++v) acc[v] = o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (act) {
+    int64_t b, e;
+    row_range(a.t.row_ptr, a.t.entries, a.t.k, i, b, e);
+    const int64_t src = a.t.score ? i * a.t.ldt - b : 0;
+    const float z = a.t.score ? a.t.logz[i] : 0.f;
     for (int64_t q = b + grp; q < e; q += NG * RF) {
       int32_t key[RF];
       float c[RF];
-      f32x4 y[RF][V];
+      f32x4 w[RF][V];
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
         const int64_t at = q + f * NG;
-        key[f] = at < e ? a.key[at] : a.items;
-        c[f] = at < e ? a.coef[at] : 0.f;
+        key[f] = at < e ? a.t.item[at + src] : -1;
+        if (key[f] >= a.t.items) key[f] = -1;
+        c[f] = 0.f;
+        if (key[f] >= 0) c[f] = a.t.score ? a.t.score[at + src] : a.t.value ? a.t.value[at] : 1.f;
       }
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) y[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (key[f] < a.items) load_row<T, G, V>(y[f], a.w.p + key[f] * a.w.ld, g, a.K, a.w.vec);
+        for (int v = 0; v < V; ++v) w[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (key[f] >= 0) load_row<T, G, V>(w[f], a.w.p + key[f] * a.w.ld, g, a.K, a.w.vec);
       }
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
-        float d = 0.f;
+        if (a.t.score) {
+          c[f] = key[f] >= 0 ? expf(c[f] / a.t.tau - z) : 0.f;
+          if (c[f] == 0.f) continue;  // no entry: what its item holds does not count
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int z = 0; z < 4; ++z) d = fmaf(x[v][z], y[f][v][z], d);
-#pragma unroll
-        for (int s = G / 2; s > 0; s >>= 1) d += __shfl_xor(d, s);
-        if (key[f] < a.items) loss = fmaf(c[f], lse - d * a.inv_tau, loss);
-        if constexpr (DX) {
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) acc[v][z] = fmaf(c[f], y[f][v][z], acc[v][z]);
-        }
+          for (int u = 0; u < 4; ++u) acc[v][u] = fmaf(c[f], w[f][v][u], acc[v][u]);
       }
     }
-  }
+    if (a.dX)
+      for (int s = grp; s < a.splits; s += NG) {
+        const float f = __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
 #pragma unroll
-  for (int s = G; s < 64; s <<= 1) {
-    loss += __shfl_xor(loss, s);
-    if constexpr (DX) {
+        for (int v = 0; v < V; ++v) {
+          const int k0 = v * 4 * G + 4 * g;
+          if (k0 >= a.ldo) continue;
+          const f32x4 u = *reinterpret_cast<const f32x4 *>(a.o + (s * a.own_pad + i) * a.ldo + k0);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) o[v][q] = fmaf(u[q], f, o[v][q]);
+        }
+      }
+#pragma unroll
+    for (int s = G; s < 64; s <<= 1)
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int z = 0; z < 4; ++z) acc[v][z] += __shfl_xor(acc[v][z], s);
-    }
+        for (int u = 0; u < 4; ++u) {
+          acc[v][u] += __shfl_xor(acc[v][u], s);
+          o[v][u] += __shfl_xor(o[v][u], s);
+        }
   }
-  if constexpr (TW == 4) {
+  if constexpr (TW > 1) {
     if (lane < G) {
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int z = 0; z < 4; ++z) part[wave][(v * 4 + z) * 64 + g] = acc[v][z];
-      if (g == 0) part[wave][64 * 4 * V] = loss;
+      for (int v = 0; v < V; ++v) {
+        part[wave][2 * v * G + g] = acc[v];
+        part[wave][(2 * v + 1) * G + g] = o[v];
+      }
     }
     __syncthreads();
     if (wave != 0) return;
-    loss = part[0][64 * 4 * V] + part[1][64 * 4 * V] + part[2][64 * 4 * V] + part[3][64 * 4 * V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      acc[v] = part[0][2 * v * G + g];
+      o[v] = part[0][(2 * v + 1) * G + g];
+      for (int w = 1; w < TW; ++w) {
+        acc[v] += part[w][2 * v * G + g];
+        o[v] += part[w][(2 * v + 1) * G + g];
+      }
+    }
+  }
+  float d = 0.f;  // x . c
+  if (act) {
+    f32x4 x[V];
+    load_row<T, G, V>(x, a.x.p + i * a.x.ld, g, a.K, a.x.vec);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        const int at = (v * 4 + z) * 64 + g;
-        acc[v][z] = part[0][at] + part[1][at] + part[2][at] + part[3][at];
-      }
+      for (int u = 0; u < 4; ++u) d = fmaf(x[v][u], acc[v][u], d);
+#pragma unroll
+    for (int s = G / 2; s > 0; s >>= 1) d += __shfl_xor(d, s);
   }
   if (lane == 0) {
-    if (a.loss) a.loss[i] = a.gain * (loss + a.extra[i]);
+    if (a.loss) a.loss[i] = act || a.t.extra[i] != 0.f ? a.t.tau * a.t.tau * (a.t.extra[i] + fmaf(a.t.total[i], lse, -d / a.t.tau)) : 0.f;
     if (a.lse) a.lse[i] = lse;
     if (a.rowvec) {
       a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 : -__builtin_inff();
-      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.share[i] / a.scal->amax : 0.f;
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.t.share[i] / a.scal->amax : 0.f;
     }
   }
-  if constexpr (DX) {
-    if (lane >= G) return;
-    const float gw = a.gw[i], mean = a.total[i] / den;
-    f32x4 o[V];
+  if (a.dX && lane < G) {
+    const float gw = a.t.gw[i], mean = ldexpf(a.t.total[i] / den, -a.scal->ew);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k0 = v * 4 * G + 4 * g;
-      o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (k0 >= a.K) continue;
-      for (int s = 0; s < a.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(a.o + (s * a.own_pad + i) * a.ldo + k0);
+      f32x4 out;
 #pragma unroll
-        for (int z = 0; z < 4; ++z) o[v][z] = fmaf(u[z], f, o[v][z]);
-      }
-      f32x4 d;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) d[z] = act ? gw * (mean * ldexpf(o[v][z], -a.scal->ew) - acc[v][z]) : 0.f;
-      store4(a.dX + i * a.lddx, k0, a.K, a.vec_out, d);
+      for (int u = 0; u < 4; ++u) out[u] = act ? gw * fmaf(mean, o[v][u], -acc[v][u]) : 0.f;
+      store4(a.dX + i * a.lddx, k0, a.K, a.vec_out, out);
     }
   }
 }
 
-// ------------------------------------------------------------------ the targets by item
-// A stable sort of the entries by item, 9 bits a pass: entries of an item stay in row order, so the
-// sums below have a fixed order.  A workgroup takes 4096 entries, a wavefront 1024 of them in order;
-// the rank of an entry among its wavefront's equal digits comes from the lanes' ballots.
-constexpr int kBits = 9, kBins = 1 << kBits, kSortTile = 4096;
+// ------------------------------------------------------------------ the targets by tiles of items
+// A stable sort of the records by their key, up to 10 bits a pass (one pass up to 32,736 items): records of a tile stay
+// in row order, which the pass over rows relies on, and nothing depends on the order of atomics.  A workgroup
+// takes 4096 records, a wavefront 1024 of them in order; the rank of a record among its wavefront's
+// equal digits comes from the lanes' ballots.  Bound by the scattered writes of the payloads.
+constexpr int kBins = 1024, kSortTile = 4096;
+static_assert(kBins == 4 * kThreads, "four digits per thread");
 
-__global__ __launch_bounds__(kThreads) void k_sort_count(const int32_t *key, int64_t n, int shift, int32_t *hist, int32_t blocks) {
+__global__ __launch_bounds__(kThreads) void k_sort_count(const int32_t *key, int64_t n, int shift, int bins, int32_t *hist, int32_t blocks) {
   __shared__ int32_t cnt[kBins];
-  for (int b = threadIdx.x; b < kBins; b += kThreads) cnt[b] = 0;
+  for (int b = threadIdx.x; b < bins; b += kThreads) cnt[b] = 0;
   __syncthreads();
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile;
+#pragma unroll 4
   for (int q = threadIdx.x; q < kSortTile; q += kThreads)
-    if (base + q < n) atomicAdd(&cnt[(key[base + q] >> shift) & (kBins - 1)], 1);
+    if (base + q < n) atomicAdd(&cnt[(key[base + q] >> shift) & (bins - 1)], 1);
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += kThreads) hist[static_cast<int64_t>(b) * blocks + blockIdx.x] = cnt[b];
+  for (int b = threadIdx.x; b < bins; b += kThreads) hist[static_cast<int64_t>(b) * blocks + blockIdx.x] = cnt[b];
 }
 
 // Exclusive sums of each digit's counts over the workgroups, and the digit's total
@@ -788,23 +899,27 @@ __global__ __launch_bounds__(kThreads) void k_sort_scan(int32_t *hist, int32_t b
   if (threadIdx.x == 0) total[blockIdx.x] = carry;
 }
 
-struct Entries {
-  int32_t *key, *row;
-  float *cb;
+struct Records {
+  int32_t *key;
+  uint2 *pay;
 };
-__global__ __launch_bounds__(kThreads) void k_sort_move(Entries in, Entries out, int64_t n, int shift, const int32_t *hist,
-                                                        int32_t blocks, const int32_t *total) {
+// first: where the digits start, for the one pass whose digits are the whole keys (NULL otherwise)
+__global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out, int64_t n, int shift, int bits, const int32_t *hist,
+                                                        int32_t blocks, const int32_t *total, int64_t *first, int32_t firsts) {
   __shared__ int32_t cnt[4][kBins], sh[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << bits;
   const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / 4);
   for (int b = threadIdx.x; b < 4 * kBins; b += kThreads) (&cnt[0][0])[b] = 0;
   __syncthreads();
+#pragma unroll 4
   for (int q = lane; q < kSortTile / 4; q += 64)
-    if (base + q < n) atomicAdd(&cnt[wave][(in.key[base + q] >> shift) & (kBins - 1)], 1);
-  // where each digit starts: the digits before it, two per thread
-  const int b0 = 2 * threadIdx.x;
-  const int32_t v0 = total[b0], v1 = total[b0 + 1];
-  int32_t s = v0 + v1;
+    if (base + q < n) atomicAdd(&cnt[wave][(in.key[base + q] >> shift) & (bins - 1)], 1);
+  // where each digit starts: the digits before it, four per thread
+  const int b0 = 4 * threadIdx.x;
+  int32_t v[4], s = 0;
+#pragma unroll
+  for (int z = 0; z < 4; ++z) s += v[z] = b0 + z < bins ? total[b0 + z] : 0;
+  const int32_t own = s;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int32_t u = __shfl_up(s, o);
@@ -812,35 +927,37 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(Entries in, Entries out,
   }
   if (lane == 63) sh[wave] = s;
   __syncthreads();
-  int32_t before = s - v0 - v1;
+  int32_t before = s - own;
   for (int w = 0; w < wave; ++w) before += sh[w];
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    int32_t at = before + (z ? v0 : 0) + hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x];
-    for (int w = 0; w < 4; ++w) {
-      const int32_t c = cnt[w][b0 + z];
-      cnt[w][b0 + z] = at;
-      at += c;
+  for (int z = 0; z < 4; ++z) {
+    if (b0 + z < bins) {
+      if (first && blockIdx.x == 0 && b0 + z < firsts) first[b0 + z] = before;
+      int32_t at = before + hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x];
+      for (int w = 0; w < 4; ++w) {
+        const int32_t c = cnt[w][b0 + z];
+        cnt[w][b0 + z] = at;
+        at += c;
+      }
     }
+    before += v[z];
   }
   __syncthreads();
   volatile int32_t *mine = cnt[wave];
   for (int q = lane; q < kSortTile / 4; q += 64) {
     const bool in_range = base + q < n;
     const int32_t key = in_range ? in.key[base + q] : 0;
-    const int d = (key >> shift) & (kBins - 1);
+    const int d = (key >> shift) & (bins - 1);
     unsigned long long same = __ballot(in_range);
-#pragma unroll
-    for (int bit = 0; bit < kBits; ++bit) {
+    for (int bit = 0; bit < bits; ++bit) {
       const unsigned long long set = __ballot((d >> bit) & 1);
       same &= (d >> bit) & 1 ? set : ~set;
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
     if (in_range) {
       const int32_t to = mine[d] + rank;
-      out.key[to] = key;
-      out.row[to] = in.row[base + q];
-      out.cb[to] = in.cb[base + q];
+      if (!first) out.key[to] = key;
+      out.pay[to] = in.pay[base + q];
     }
     __builtin_amdgcn_wave_barrier();
     if (in_range && rank == 0) mine[d] += __popcll(same);
@@ -848,14 +965,22 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(Entries in, Entries out,
   }
 }
 
+// Where the records of each tile start, after more than one sorting pass
+__global__ __launch_bounds__(kThreads) void k_first(const int32_t *key, int64_t n, int64_t *first, int32_t firsts) {
+  const int32_t t = blockIdx.x * kThreads + threadIdx.x;
+  if (t >= firsts) return;
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (key[mid] < t) lo = mid + 1; else hi = mid;
+  }
+  first[t] = lo;
+}
+
 template <class T>
 struct ItemArgs {
-  int64_t own_pad, entries, chunk, chunks;  // chunk: entries that one lane group sums
-  int32_t items, K, ldo, splits, kd;
-  Table<T> x;
-  Entries ent;
-  float *part;  // [2 chunks][32 kd] sums of a chunk's first and last item
-  float *ysum;  // [items][32 kd] sums of items whose entries lie inside one chunk
+  int64_t own_pad;
+  int32_t items, K, ldo, splits;
   const Scal *scal;
   const float *m, *o;
   T *dW;
@@ -863,114 +988,35 @@ struct ItemArgs {
   bool vec_out;
 };
 
-// sum cb x_row of every item's entries, the sorted list cut into chunks: a chunk's first and last item may go on
-// in the neighbours, so their sums are kept apart.  Bound by the gathers of x rows.
-template <class T, int G, int V>
-__global__ __launch_bounds__(kThreads) void k_item_lists(ItemArgs<T> a) {
-  constexpr int RF = 4;
-  const int g = threadIdx.x & (G - 1);
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * (kThreads / G) + threadIdx.x / G;
-  if (c >= a.chunks) return;
-  const int64_t b = c * a.chunk, e = min(b + a.chunk, a.entries);
-  const int ld = a.kd * 32;
-  f32x4 acc[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int32_t cur = a.ent.key[b];
-  bool first = true;
-  auto put = [&](float *to) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int k0 = v * 4 * G + 4 * g;
-      if (k0 < ld) *reinterpret_cast<f32x4 *>(to + k0) = acc[v];
-      acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  };
-  for (int64_t q = b; q < e; q += RF) {
-    int32_t key[RF];
-    float cb[RF];
-    f32x4 x[RF][V];
-#pragma unroll
-    for (int f = 0; f < RF; ++f) {
-      const bool in = q + f < e;
-      key[f] = in ? a.ent.key[q + f] : a.items;
-      cb[f] = in && key[f] < a.items ? a.ent.cb[q + f] : 0.f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) x[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (in && key[f] < a.items) load_row<T, G, V>(x[f], a.x.p + a.ent.row[q + f] * a.x.ld, g, a.K, a.x.vec);
-    }
-#pragma unroll
-    for (int f = 0; f < RF; ++f) {
-      if (q + f < e && key[f] != cur) {
-        if (first) {
-          put(a.part + 2 * c * ld);
-          first = false;
-        } else {
-          put(a.ysum + static_cast<int64_t>(cur) * ld);
-        }
-        cur = key[f];
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int z = 0; z < 4; ++z) acc[v][z] = fmaf(cb[f], x[f][v][z], acc[v][z]);
-    }
-  }
-  put(a.part + (2 * c + (first ? 0 : 1)) * ld);
-}
-
-__device__ inline int64_t lower(const int32_t *key, int64_t n, int32_t j) {
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (key[mid] < j) lo = mid + 1; else hi = mid;
-  }
-  return lo;
-}
-
-// dW_j: the passes' pieces joined, minus the targets' sums
+// dW_j: the passes' pieces joined.  Bound by memory.
 template <class T, int G, int V>
 __global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
   const int g = threadIdx.x & (G - 1);
   const int64_t j = static_cast<int64_t>(blockIdx.x) * (kThreads / G) + threadIdx.x / G;
   if (j >= a.items) return;
-  const int ld = a.kd * 32;
-  f32x4 o[V], y[V];
+  const float back = a.splits ? ldexpf(a.scal->amax, -a.scal->ex) : 0.f;
+  f32x4 o[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) o[v] = y[v] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto add = [&](f32x4 (&to)[V], const float *from, float f) {
+  for (int v = 0; v < V; ++v) o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f(a.m[s * a.own_pad + j] - kShift);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k0 = v * 4 * G + 4 * g;
-      if (k0 >= ld) continue;
-      const f32x4 u = *reinterpret_cast<const f32x4 *>(from + k0);
+      if (k0 >= a.ldo) continue;
+      const f32x4 u = *reinterpret_cast<const f32x4 *>(a.o + (s * a.own_pad + j) * a.ldo + k0);
 #pragma unroll
-      for (int z = 0; z < 4; ++z) to[v][z] = fmaf(u[z], f, to[v][z]);
-    }
-  };
-  for (int s = 0; s < a.splits; ++s)
-    add(o, a.o + (s * a.own_pad + j) * a.ldo, __builtin_amdgcn_exp2f(a.m[s * a.own_pad + j] - kShift));
-  if (a.entries > 0) {
-    const int64_t lo = lower(a.ent.key, a.entries, static_cast<int32_t>(j)), hi = lower(a.ent.key, a.entries, static_cast<int32_t>(j) + 1);
-    if (hi > lo) {
-      const int64_t c0 = lo / a.chunk, c1 = (hi - 1) / a.chunk;
-      const bool from_start = lo == c0 * a.chunk;
-      if (c0 == c1 && !from_start && hi != min((c0 + 1) * a.chunk, a.entries)) {
-        add(y, a.ysum + j * ld, 1.f);
-      } else {
-        add(y, a.part + (2 * c0 + (from_start ? 0 : 1)) * ld, 1.f);
-#pragma unroll 4
-        for (int64_t c = c0 + 1; c <= c1; ++c) add(y, a.part + 2 * c * ld, 1.f);
-      }
+      for (int z = 0; z < 4; ++z) o[v][z] = fmaf(u[z], f, o[v][z]);
     }
   }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    f32x4 d;
     const int k0 = v * 4 * G + 4 * g;
     if (k0 >= a.K) continue;
+    f32x4 d;
 #pragma unroll
-    for (int z = 0; z < 4; ++z) d[z] = (a.splits ? ldexpf(o[v][z], -a.scal->ex) * a.scal->amax : 0.f) - y[v][z];
+    for (int z = 0; z < 4; ++z) d[z] = o[v][z] * back;
     store4(a.dW + j * a.lddw, k0, a.K, a.vec_out, d);
   }
 }
@@ -1272,9 +1318,8 @@ struct Plan {
   int64_t x_stride, w_stride;  // halves per tile
   int32_t rsplits, csplits;
   int64_t rper, cper;          // tiles per split
-  int64_t chunk, chunks;
-  int32_t sort_blocks, passes;
-  int64_t key[2], row[2], cb[2], coef, act, total, extra, share, gw, row_part, part, scal, px, pw, m, l, o, rowvec, hist, bins, isum, ysum;
+  int32_t sort_blocks, passes, bits;  // of the sort: bits of a pass
+  int64_t key[2], pay[2], act, total, extra, share, gw, logz, row_part, part, scal, px, pw, m, l, o, rowvec, hist, bins, first;
   int64_t bytes;
 };
 
@@ -1319,25 +1364,22 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
     p.cper = up(p.xt, p.csplits);
     p.csplits = static_cast<int32_t>(up(p.xt, p.cper));
   }
-  // a lane group sums 32 entries, more where 16,384 groups would not cover them
-  p.chunk = 32;
-  while (p.chunk < 1024 && up(entries, p.chunk) > 16384) p.chunk *= 2;
-  p.chunks = up(entries, p.chunk);
   p.sort_blocks = static_cast<int32_t>(up(entries, kSortTile));
-  p.passes = 0;
-  for (int64_t v = h->items; v > 0; v >>= kBits) ++p.passes;
+  int32_t bits = 0;
+  for (int64_t v = p.wt; v > 0; v >>= 1) ++bits;  // keys 0 .. tiles
+  p.passes = (bits + 9) / 10;
+  p.bits = (bits + p.passes - 1) / p.passes;
   Arena a;
   for (int q = 0; q < 2; ++q) {
-    p.key[q] = a.take(entries * 4);
-    p.row[q] = a.take(dw ? entries * 4 : 0);
-    p.cb[q] = a.take(dw ? entries * 4 : 0);
+    p.key[q] = a.take(dw ? entries * 4 : 0);
+    p.pay[q] = a.take(dw ? entries * 8 : 0);
   }
-  p.coef = a.take(entries * 4);
   p.act = a.take(n * 4);
   p.total = a.take(n * 4);
   p.extra = a.take(n * 4);
   p.share = a.take(n * 4);
   p.gw = a.take(n * 4);
+  p.logz = a.take(n * 4);
   p.row_part = a.take(kRowParts * 4);
   p.part = a.take(2 * kParts * 4);
   p.scal = a.take(sizeof(Scal));
@@ -1350,8 +1392,7 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   p.rowvec = a.take(dw ? p.xt * 64 * 4 : 0);
   p.hist = a.take(dw ? static_cast<int64_t>(p.sort_blocks) * kBins * 4 : 0);
   p.bins = a.take(kBins * 4);
-  p.isum = a.take(dw ? 2 * p.chunks * p.kd * 32 * 4 : 0);
-  p.ysum = a.take(dw && entries ? (h->items + 1) * p.kd * 32 * 4 : 0);
+  p.first = a.take(dw ? (p.wt + 1) * 8 : 0);
   p.bytes = a.at;
   return p;
 }
@@ -1360,8 +1401,8 @@ template <int NP, int KC, int DB>
 void launch_pass(PassArgs a, bool col, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(up(a.own_tiles, kWaves) * a.splits));
   const int bytes = stage_of(NP, KC, DB, col).halves * 2;
-  a.buffers = 2 * bytes <= kLds ? 2 : 1;
-  const unsigned lds = static_cast<unsigned>(a.buffers * bytes);
+  a.buffers = 2 * bytes + (col ? kWaves * kHalfTile * 4 : 0) <= kLds ? 2 : 1;
+  const unsigned lds = static_cast<unsigned>(a.buffers * bytes + (col ? kWaves * kHalfTile * 4 : 0));
   if (col) {
     if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64 * kWaves), lds, s, a);
   } else {
@@ -1393,25 +1434,12 @@ void run_pass(const PassArgs &a, int k16, bool col, bool sums, hipStream_t s) {
 }
 
 template <class T, int G, int V>
-void run_rows(const RowArgs<T> &a, bool dx, bool few, hipStream_t s) {
-  const int64_t rows = a.rowvec ? up(a.n, kTile) * kTile : a.n;
-  if (few) {
-    const dim3 grid(static_cast<unsigned>(rows));
-    if (dx) hipLaunchKernelGGL((k_row_finish<T, G, V, 4, true>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_row_finish<T, G, V, 4, false>), grid, dim3(kThreads), 0, s, a);
-  } else {
-    const dim3 grid(static_cast<unsigned>(up(rows, 4)));
-    if (dx) hipLaunchKernelGGL((k_row_finish<T, G, V, 1, true>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((k_row_finish<T, G, V, 1, false>), grid, dim3(kThreads), 0, s, a);
-  }
-}
-
-template <class T, int G, int V>
-void run_items(const ItemArgs<T> &a, hipStream_t s) {
-  constexpr int per = kThreads / G;
-  if (a.entries > 0)
-    hipLaunchKernelGGL((k_item_lists<T, G, V>), dim3(static_cast<unsigned>(up(a.chunks, per))), dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL((k_item_finish<T, G, V>), dim3(static_cast<unsigned>(up(a.items, per))), dim3(kThreads), 0, s, a);
+void run_rows(const RowArgs<T> &a, hipStream_t s) {
+  const int64_t rows = a.rowvec ? up(a.t.n, kTile) * kTile : a.t.n;
+  // wavefronts per row: all that 256 CUs hold, for lists long enough
+  if (a.t.n <= 256) hipLaunchKernelGGL((k_row_finish<T, G, V, 16>), dim3(static_cast<unsigned>(rows)), dim3(1024), 0, s, a);
+  else if (a.t.n <= 2048) hipLaunchKernelGGL((k_row_finish<T, G, V, 4>), dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_row_finish<T, G, V, 1>), dim3(static_cast<unsigned>(up(rows, 4))), dim3(kThreads), 0, s, a);
 }
 
 // Lanes per row: 4 numbers each, 8 above 256
@@ -1440,22 +1468,22 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
   hipStream_t s = h->stream;
   Scal *scal = reinterpret_cast<Scal *>(base + p.scal);
   t.items = static_cast<int32_t>(h->items);
-  t.key = at_i(p.key[0]);
-  t.erow = at_i(p.row[0]);
-  t.coef = at_f(p.coef);
-  t.cb = dw ? at_f(p.cb[0]) : nullptr;
+  t.dead = static_cast<int32_t>(p.wt);
+  t.key = dw ? at_i(p.key[0]) : nullptr;
+  t.pay = reinterpret_cast<uint2 *>(base + p.pay[0]);
   t.act = at_i(p.act);
   t.total = at_f(p.total);
   t.extra = at_f(p.extra);
   t.share = at_f(p.share);
   t.gw = at_f(p.gw);
+  t.logz = at_f(p.logz);
   t.part = at_f(p.row_part);
   Table<T> x{X, ldx, t.n, aligned4(X, ldx), t.act}, w{W, ldw, h->items, aligned4(W, ldw), nullptr};
   _Float16 *px = reinterpret_cast<_Float16 *>(base + p.px), *pw = reinterpret_cast<_Float16 *>(base + p.pw);
   const float scale = 1.44269504088896340736f / t.tau;
   if (t.n > 0) {
     if (t.row_ptr && dw && t.entries > 0)
-      hipLaunchKernelGGL(k_fill_keys, dim3(blocks_for(t.entries, kThreads * 4, 4096)), dim3(kThreads), 0, s, t.key, t.entries, t.items);
+      hipLaunchKernelGGL(k_fill_keys, dim3(blocks_for(t.entries, kThreads * 4, 4096)), dim3(kThreads), 0, s, t.key, t.entries, t.dead);
     const unsigned row_blocks = blocks_for(t.n, 4, kRowParts);
     hipLaunchKernelGGL((k_targets<Distill>), dim3(row_blocks), dim3(kThreads), 0, s, t);
     hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kThreads), 0, s, x, w, h->K, at_f(p.part));
@@ -1479,37 +1507,43 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     a.o = at_f(p.o);
     run_pass<NP>(a, p.k16, false, dx, s);
     RowArgs<T> r{};
-    r.n = t.n;
-    r.entries = t.entries;
+    r.t = t;
     r.own_pad = p.xt * kTile;
     r.K = h->K;
     r.ldo = p.kd * 32;
-    r.k = t.k;
     r.splits = p.rsplits;
-    r.items = t.items;
-    r.row_ptr = t.row_ptr;
     r.x = x;
     r.w = w;
-    r.key = t.key;
-    r.coef = t.coef;
-    r.total = t.total;
-    r.extra = t.extra;
-    r.share = t.share;
-    r.gw = t.gw;
     r.scal = scal;
     r.m = a.m;
     r.l = a.l;
     r.o = a.o;
-    r.inv_tau = 1.f / t.tau;
-    r.gain = t.tau * t.tau;
     r.loss = loss;
     r.lse = lse;
     r.dX = dX;
     r.lddx = lddx;
     r.vec_out = dx && aligned4(dX, lddx);
     r.rowvec = dw ? at_f(p.rowvec) : nullptr;
-    by_k(h->K, [&](auto g, auto v) { run_rows<T, g(), v()>(r, dx, t.n <= 1024, s); });
+    by_k(h->K, [&](auto g, auto v) { run_rows<T, g(), v()>(r, s); });
     if (dw) {
+      Records rec[2];
+      for (int q = 0; q < 2; ++q) rec[q] = Records{at_i(p.key[q]), reinterpret_cast<uint2 *>(base + p.pay[q])};
+      int64_t *first = reinterpret_cast<int64_t *>(base + p.first);
+      const int32_t firsts = static_cast<int32_t>(p.wt + 1);
+      int from = 0;
+      if (t.entries > 0) {
+        for (int q = 0; q < p.passes; ++q, from ^= 1) {
+          const dim3 blocks(static_cast<unsigned>(p.sort_blocks));
+          hipLaunchKernelGGL(k_sort_count, blocks, dim3(kThreads), 0, s, rec[from].key, t.entries, q * p.bits, 1 << p.bits, at_i(p.hist),
+                             p.sort_blocks);
+          hipLaunchKernelGGL(k_sort_scan, dim3(1 << p.bits), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
+          hipLaunchKernelGGL(k_sort_move, blocks, dim3(kThreads), 0, s, rec[from], rec[from ^ 1], t.entries, q * p.bits, p.bits,
+                             at_i(p.hist), p.sort_blocks, at_i(p.bins), p.passes == 1 ? first : nullptr, firsts);
+        }
+        if (p.passes > 1)
+          hipLaunchKernelGGL(k_first, dim3(static_cast<unsigned>(up(firsts, kThreads))), dim3(kThreads), 0, s, rec[from].key, t.entries, first,
+                             firsts);
+      }
       a.own = pw;
       a.own_stride = p.w_stride;
       a.own_tiles = p.wt;
@@ -1519,42 +1553,27 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       a.str_rows = t.n;
       a.rowvec = at_f(p.rowvec);
       a.tiles_per_split = p.cper;
+      a.first = t.entries > 0 ? first : nullptr;
+      a.pay = rec[from].pay;
       run_pass<NP>(a, p.k16, true, true, s);
     }
   }
   if (dw) {
     ItemArgs<T> a{};
-    int from = 0;
-    Entries ent[2] = {{at_i(p.key[0]), at_i(p.row[0]), at_f(p.cb[0])}, {at_i(p.key[1]), at_i(p.row[1]), at_f(p.cb[1])}};
-    if (t.n > 0 && t.entries > 0) {
-      for (int q = 0; q < p.passes; ++q, from ^= 1) {
-        const unsigned blocks = static_cast<unsigned>(p.sort_blocks);
-        hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(kThreads), 0, s, ent[from].key, t.entries, q * kBits, at_i(p.hist), p.sort_blocks);
-        hipLaunchKernelGGL(k_sort_scan, dim3(kBins), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
-        hipLaunchKernelGGL(k_sort_move, dim3(blocks), dim3(kThreads), 0, s, ent[from], ent[from ^ 1], t.entries, q * kBits, at_i(p.hist),
-                           p.sort_blocks, at_i(p.bins));
-      }
-    }
     a.own_pad = p.wt * kTile;
-    a.entries = t.n > 0 ? t.entries : 0;
-    a.chunk = p.chunk;
-    a.chunks = p.chunks;
     a.items = t.items;
     a.K = h->K;
     a.ldo = p.kd * 32;
     a.splits = t.n > 0 ? p.csplits : 0;
-    a.kd = p.kd;
-    a.x = x;
-    a.ent = ent[from];
-    a.part = at_f(p.isum);
-    a.ysum = at_f(p.ysum);
     a.scal = scal;
     a.m = at_f(p.m);
     a.o = at_f(p.o);
     a.dW = dW;
     a.lddw = lddw;
     a.vec_out = aligned4(dW, lddw);
-    by_k(h->K, [&](auto g, auto v) { run_items<T, g(), v()>(a, s); });
+    by_k(h->K, [&](auto g, auto v) {
+      hipLaunchKernelGGL((k_item_finish<T, g(), v()>), dim3(static_cast<unsigned>(up(h->items, kThreads / g()))), dim3(kThreads), 0, s, a);
+    });
   }
   SOFT_TRY(h, hipGetLastError());
   return PS_SOFT_OK;
@@ -1620,10 +1639,11 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
   return PS_SOFT_OK;
 }
 
-constexpr int64_t kMaxRows = (1LL << 31) - 65;
+constexpr int64_t kMaxRows = 1LL << 26;             // a record holds 32 row + item mod 32 in 32 bits
+constexpr int64_t kMaxItems = (1LL << 31) - 65, kMaxEntries = (1LL << 31) - 65;
 
 int check_tables(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void *W, int64_t ldw) {
-  if (n < 0 || n > kMaxRows) return fail(h, PS_SOFT_EINVAL, "rows must be in [0, 2^31 - 65], not %lld", (long long)n);
+  if (n < 0 || n > kMaxRows) return fail(h, PS_SOFT_EINVAL, "rows must be in [0, 2^26], not %lld", (long long)n);
   if ((n > 0 && !X) || !W) return fail(h, PS_SOFT_EINVAL, "null table");
   if (ldx < h->K || ldw < h->K) return fail(h, PS_SOFT_EINVAL, "row strides must be at least K = %d", h->K);
   return PS_SOFT_OK;
@@ -1631,7 +1651,7 @@ int check_tables(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void
 
 int check_outputs(ps_soft_t *h, const void *dX, int64_t lddx, const void *dW, int64_t lddw, int64_t entries) {
   if ((dX && lddx < h->K) || (dW && lddw < h->K)) return fail(h, PS_SOFT_EINVAL, "gradients' row strides must be at least K = %d", h->K);
-  if (entries < 0 || entries > kMaxRows) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
+  if (entries < 0 || entries > kMaxEntries) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
   return PS_SOFT_OK;
 }
 
@@ -1661,7 +1681,7 @@ extern "C" {
 int ps_soft_create(int64_t items, int32_t K, int32_t type, ps_soft_t **out) {
   if (!out) return PS_SOFT_EINVAL;
   *out = nullptr;
-  if (items < 1 || items > kMaxRows || K < 1 || K > kMaxK || type < PS_SOFT_F32 || type > PS_SOFT_F16) return PS_SOFT_EINVAL;
+  if (items < 1 || items > kMaxItems || K < 1 || K > kMaxK || type < PS_SOFT_F32 || type > PS_SOFT_F16) return PS_SOFT_EINVAL;
   ps_soft_t *h = new (std::nothrow) ps_soft_t();
   if (!h) return PS_SOFT_ENOMEM;
   h->items = items;
@@ -1711,8 +1731,8 @@ int ps_soft_set_stream(ps_soft_t *h, void *hip_stream) {
 
 int ps_soft_reserve(ps_soft_t *h, int64_t n, int64_t entries, int32_t top) {
   if (!h) return PS_SOFT_EINVAL;
-  if (n < 0 || n > kMaxRows || entries < 0 || entries > kMaxRows || top < 0 || top > kMaxTop)
-    return fail(h, PS_SOFT_EINVAL, "rows and entries must be in [0, 2^31 - 65], top in [0, %d]", kMaxTop);
+  if (n < 0 || n > kMaxRows || entries < 0 || entries > kMaxEntries || top < 0 || top > kMaxTop)
+    return fail(h, PS_SOFT_EINVAL, "rows must be in [0, 2^26], entries in [0, 2^31 - 65], top in [0, %d]", kMaxTop);
   DeviceGuard guard;
   const int rc = open(h, guard);
   if (rc) return rc;
@@ -1750,7 +1770,7 @@ int ps_soft_distill(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const v
   if (k < 1 || ldt < k) return fail(h, PS_SOFT_EINVAL, "teacher's lists: k = %d, stride %lld", k, (long long)ldt);
   if (!(tau > 0) || !std::isfinite(tau)) return fail(h, PS_SOFT_EINVAL, "tau must be positive and finite");
   if (n > 0 && (!item || !score)) return fail(h, PS_SOFT_EINVAL, "null teacher's lists");
-  if ((rc = check_outputs(h, dX, lddx, dW, lddw, n > kMaxRows / k ? kMaxRows + 1 : n * k))) return rc;
+  if ((rc = check_outputs(h, dX, lddx, dW, lddw, n * k))) return rc;
   Targets t{};
   t.n = n;
   t.entries = n * k;
@@ -1770,7 +1790,7 @@ int ps_soft_top(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void 
   int rc = check_tables(h, n, X, ldx, W, ldw);
   if (rc) return rc;
   if (k < 1 || k > kMaxTop || ldo < k) return fail(h, PS_SOFT_EINVAL, "k must be in [1, %d] and the outputs' stride at least k", kMaxTop);
-  if (entries < 0 || entries > kMaxRows) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
+  if (entries < 0 || entries > kMaxEntries) return fail(h, PS_SOFT_EINVAL, "entries must be in [0, 2^31 - 65], not %lld", (long long)entries);
   if (row_ptr && entries > 0 && !item) return fail(h, PS_SOFT_EINVAL, "null item list");
   if (n > 0 && (!top_item || !top_score)) return fail(h, PS_SOFT_EINVAL, "null outputs");
   if (n == 0) return PS_SOFT_OK;

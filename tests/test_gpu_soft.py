@@ -127,6 +127,25 @@ def test_xent_lists(soft, n, M, K, mean, splits, dtype):
     check("no values", ones, want, bounds, dtype)
 
 
+def test_xent_the_same_item_many_times(soft):
+    # rows that list an item two to nine times, dense lists, values of either sign: added in the list's order
+    n, M, K = 150, 45, 24
+    g = gen(20)
+    X, W = tables(n, M, K, F32, g)
+    item = torch.randint(0, M, (n, 90), generator=g, dtype=torch.int32)
+    item[:, 5:9] = item[:, 4:5]
+    ptr = torch.arange(0, 90 * n + 1, 90).cuda()
+    item = item.flatten().cuda()
+    value = torch.randn(item.shape, generator=g).cuda()
+    want, bounds = soft_ref.xent(X, W, item, ptr, value)
+    say("xent many times")
+    with soft.PsSoft(M, K) as h:
+        got = h.xent(X, W, item, row_ptr=ptr, value=value)
+        again = h.xent(X, W, item, row_ptr=ptr, value=value)
+    check("many times", got, want, bounds, F32)
+    assert same(got, again)
+
+
 def test_xent_items_of_many_digits_and_popular_items(soft):
     # items beyond 2^18 take three sorting passes; one item in every row's list goes over many chunks
     n, M, K = 3000, 300_000, 8
