@@ -26,6 +26,7 @@
 #include <cstdio>
 #include <new>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "ps_soft.h"
@@ -733,10 +734,12 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   }
   const bool act = a.t.act[i];
   float top = kNone;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.m[s * a.own_pad + i]);
+  for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, a.m[s * a.own_pad + i]);
+  top = wave_max(top);
   float den = 0.f;
-  for (int s = 0; s < a.splits; ++s)
+  for (int s = lane; s < a.splits; s += 64)
     den += a.l[s * a.own_pad + i] * __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
+  den = wave_sum(den);
   const float lse2 = top - kShift + log2f(den);
   const float lse = lse2 * 0.69314718055994530942f;
   f32x4 acc[V], o[V];
@@ -1086,33 +1089,92 @@ __device__ inline void best_add(Best b, int k, bool want, uint64_t key, int32_t 
   __syncthreads();
 }
 
+// A score in 64 bits: products of the tables' numbers are exact, and the sum has one order everywhere: 8 lanes of 4
+// numbers each take every eighth 4, then the lanes are added in pairs.
+constexpr int kDotLanes = 8;
+template <class T>
+__device__ inline double dot64(const double *x, const T *w, int l, int K, bool vec) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int k = 4 * l; k < K; k += 4 * kDotLanes) {
+    const f32x4 v = load4(w, k, K, vec);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);
+  }
+#pragma unroll
+  for (int o = 1; o < kDotLanes; o <<= 1) s += __shfl_xor(s, o);
+  return s;
+}
+
 template <class T>
 struct TopArgs {
   int64_t row0, n;  // rows of this launch
   int32_t items, K, k, words;
   Table<T> x, w;
   const uint32_t *excluded;  // [n][words] bits (NULL: none)
+  // in pieces of the items, joined afterwards
   int64_t per_piece;
   int32_t pieces;
   uint64_t *key;   // [n][pieces][k]
   int32_t *item;
+  // or from candidates
+  const int32_t *found, *count;  // [n][room], [n]: more than room: all items
+  int32_t room;
   int32_t *out_item;
   float *out_score;
   int64_t ldo;
 };
 
-template <class T>
-__device__ inline double dot64(const double *x, const T *w, int K, bool vec) {
-  double s = 0.0;
-  for (int k = 0; k < K; k += 4) {
-    const f32x4 v = load4(w, k, K, vec);
-#pragma unroll
-    for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);  // products are exact
+// 256 scores, an item per thread: 8 lanes make 8 items' in turn.  item_of(q): the q-th item or -1
+template <class T, class F>
+__device__ inline void top_batch(const TopArgs<T> &a, const double *x, Best b, uint64_t &least, F item_of) {
+  const int l = threadIdx.x & (kDotLanes - 1), first = threadIdx.x & ~(kDotLanes - 1);
+  int32_t mine = -1;
+  uint64_t key = 0;
+#pragma unroll 2
+  for (int q = 0; q < kDotLanes; ++q) {
+    const int32_t j = item_of(first + q);
+    if (j < 0) continue;  // the same for the 8 lanes
+    const double s = dot64(x, a.w.p + j * a.w.ld, l, a.K, a.w.vec);
+    if (l == q) {
+      mine = j;
+      key = order_key(s);
+    }
   }
-  return s;
+  best_add(b, a.k, mine >= 0, key, mine, least);
 }
 
-// The k best of a piece of the items for one row: an item per thread
+template <class T>
+__device__ inline void top_row(const TopArgs<T> &a, int64_t r, double *x, int32_t *count) {
+  const T *xr = a.x.p + (a.row0 + r) * a.x.ld;
+  for (int k = threadIdx.x; k < kMaxK; k += kThreads) x[k] = k < a.K ? static_cast<double>(to_f(xr[k])) : 0.0;
+  if (threadIdx.x == 0) *count = 0;
+  __syncthreads();
+}
+
+template <class T>
+__device__ inline void top_all(const TopArgs<T> &a, int64_t r, const double *x, Best b, int64_t j0, int64_t j1) {
+  uint64_t least = 0;
+  for (int64_t base = j0; base < j1; base += kThreads)
+    top_batch(a, x, b, least, [&](int q) {
+      const int64_t j = base + q;
+      if (j >= j1 || (a.excluded && ((a.excluded[r * a.words + (j >> 5)] >> (j & 31)) & 1))) return -1;
+      return static_cast<int32_t>(j);
+    });
+  best_cut(b, a.k);
+}
+
+template <class T>
+__device__ inline void top_out(const TopArgs<T> &a, int64_t r, Best b) {
+  const int64_t to = (a.row0 + r) * a.ldo;
+  for (int q = threadIdx.x; q < a.k; q += kThreads) {
+    const bool there = q < *b.count;
+    a.out_item[to + q] = there ? b.item[q] : -1;
+    a.out_score[to + q] = there ? static_cast<float>(key_value(b.key[q])) : -__builtin_inff();
+  }
+}
+
+// The k best of a piece of the items for one row.  Bound by the reads of the items' rows.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_top_scan(TopArgs<T> a) {
   __shared__ double x[kMaxK];
@@ -1120,22 +1182,11 @@ __global__ __launch_bounds__(kThreads) void k_top_scan(TopArgs<T> a) {
   __shared__ int32_t items[kTopRoom], count;
   const int64_t r = blockIdx.x;
   const int piece = blockIdx.y;
-  const T *xr = a.x.p + (a.row0 + r) * a.x.ld;
-  for (int k = threadIdx.x; k < kMaxK; k += kThreads) x[k] = k < a.K ? static_cast<double>(to_f(xr[k])) : 0.0;
-  if (threadIdx.x == 0) count = 0;
-  __syncthreads();
   const Best b{keys, items, &count};
-  uint64_t least = 0;
+  top_row(a, r, x, &count);
   const int64_t j0 = piece * a.per_piece, j1 = min(j0 + a.per_piece, static_cast<int64_t>(a.items));
-  for (int64_t base = j0; base < j1; base += kThreads) {
-    const int64_t j = base + threadIdx.x;
-    bool want = j < j1;
-    if (want && a.excluded) want = !((a.excluded[r * a.words + (j >> 5)] >> (j & 31)) & 1);
-    uint64_t key = 0;
-    if (want) key = order_key(dot64(x, a.w.p + j * a.w.ld, a.K, a.w.vec));
-    best_add(b, a.k, want, key, static_cast<int32_t>(j), least);
-  }
-  best_cut(b, a.k);
+  top_all(a, r, x, b, j0, j1);
+  if (a.pieces == 1) return top_out(a, r, b);
   const int64_t to = (r * a.pieces + piece) * a.k;
   for (int q = threadIdx.x; q < a.k; q += kThreads) {
     a.key[to + q] = q < count ? keys[q] : 0;
@@ -1159,11 +1210,325 @@ __global__ __launch_bounds__(kThreads) void k_top_join(TopArgs<T> a) {
     best_add(b, a.k, j >= 0, q < all ? a.key[from + q] : 0, j, least);
   }
   best_cut(b, a.k);
-  const int64_t to = (a.row0 + r) * a.ldo;
-  for (int q = threadIdx.x; q < a.k; q += kThreads) {
-    a.out_item[to + q] = q < count ? items[q] : -1;
-    a.out_score[to + q] = q < count ? static_cast<float>(key_value(keys[q])) : -__builtin_inff();
+  top_out(a, r, b);
+}
+
+// ---- many rows: candidates by matrix instructions
+//
+// Scores of fp16 numbers (one plane) are off by at most e_ij = c (|x_i| + 1)(|w_j| + 1) of the scaled tables, and
+// that product is one more number of each row: with |w| there and -|x| here the score comes out as a lower
+// bound of the true one, with +|x| as an upper bound.  A first pass keeps the largest lower bound of every 16
+// items; the k-th largest of those, T, is below at least k true scores.  A second pass finds the items whose
+// upper bound is not below T: all of the k best are among them, and few others (about 1.2 k of 17,770 normal
+// scores at K = 128).  These are then scored in 64 bits and put in order.  A row with more candidates
+// than its room (far more equal scores than that, rows of zeros, numbers that are not finite) looks at
+// all items in 64 bits.
+//
+// c: with x' = fp16(x): |x' - x| <= 2^-11 |x| + 2^-25, so products add up to at most (2^-10 + 2^-22) |x||w| (nothing
+// for tables of 16 bits) + 2^-24 sqrt(K) (|x| + |w|), and the instruction's sums of 2 KC groups, counted at
+// 2^-22 each, to (2 KC + 16) 2^-22 |x||w|.
+constexpr int kScoreTiles = 2;   // tiles of 32 items that a step stages
+constexpr int row_room(int kc) { return kc > 25 ? 16 : 32; }  // candidates of a row that a workgroup keeps in LDS
+constexpr int kCandidates = 1024;
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_top_pack(Table<T> x, Table<T> w, int64_t row0, int64_t rows, int32_t xt, _Float16 *px, _Float16 *pw,
+                                                       int32_t K, int32_t kc, float c, const float *part, int32_t *count) {
+  extern __shared__ float tile[];
+  __shared__ float sh[4], norm[kTile];
+  const bool second = static_cast<int32_t>(blockIdx.x) >= xt;
+  const Table<T> t = second ? w : x;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) - (second ? xt : 0);
+  int ex = 0;
+  if constexpr (!std::is_same<T, f16_t>::value) ex = scale_exp(block_max(part[(second ? kParts : 0) + threadIdx.x], sh));
+  const int64_t begin = second ? 0 : row0, end = second ? t.rows : row0 + rows;
+  // a tile: kc fragments, and one more of rows' tiles, the last number's chunk with that number negated
+  _Float16 *out = second ? pw + at * kc * kFrag : px + at * (kc + 1) * kFrag;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int kd = (K + 31) / 32, wide = min(kd, kPackBlocks), ld = wide * 32 + 1;
+  const int last = K / 16;  // the chunk of the bound's number
+  float sum = 0.f;
+  int b0 = 0;
+  for (;; b0 += wide) {
+    const int nb = min(wide, kd - b0), per = nb * 8;
+    __syncthreads();
+    for (int q = threadIdx.x; q < kTile * per; q += kThreads) {
+      const int r = q / per, k0 = (q - r * per) * 4;
+      const int64_t row = begin + at * kTile + r;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (row < end && b0 * 32 + k0 < K) v = load4(t.p + row * t.ld, b0 * 32 + k0, K, t.vec);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) tile[r * ld + k0 + z] = ldexpf(v[z], ex);
+    }
+    __syncthreads();
+    for (int k = threadIdx.x & 7; k < nb * 32; k += 8) {
+      const float v = tile[(threadIdx.x >> 3) * ld + k];
+      sum = fmaf(v, v, sum);
+    }
+    for (int f = 2 * b0 + wave; f < min(2 * (b0 + nb), last); f += 4) {
+      h8 hi;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) hi[i] = static_cast<_Float16>(tile[l32 * ld + (f - 2 * b0) * 16 + half * 8 + i]);
+      *reinterpret_cast<h8 *>(out + f * kFrag + lane * 8) = hi;
+    }
+    if (b0 + nb >= kd) break;
   }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 7) == 0) {
+    const int r = threadIdx.x >> 3;
+    // rounded up: 2^-9 for the sum, the root and fp16
+    norm[r] = (sqrtf(sum) + 1.f) * (1.f + 0x1p-9f) * (second ? c * 64.f : 1.f / 64.f);
+    const int64_t row = at * kTile + r;
+    if (!second && row < rows) count[row] = sum < __builtin_inff() ? 0 : 1 << 30;
+  }
+  __syncthreads();
+  for (int f = last + wave; f <= kc; f += 4) {
+    if (f == kc && second) break;
+    const int from = f == kc ? last : f;
+    h8 hi;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = from * 16 + half * 8 + i;
+      float v = k < K ? tile[l32 * ld + k - 32 * b0] : 0.f;
+      if (k == K) v = f == kc ? -norm[l32] : norm[l32];
+      hi[i] = static_cast<_Float16>(v);
+    }
+    *reinterpret_cast<h8 *>(out + f * kFrag + lane * 8) = hi;
+  }
+}
+
+struct ScoreArgs {
+  const _Float16 *own, *str;
+  int64_t rows, own_tiles, tiles, steps_per_split;
+  int32_t items, splits, words, last;  // last: the chunk of the bound's number
+  const uint32_t *excluded;
+  float *most;        // [rows][4 steps] first pass: largest lower bounds
+  int64_t steps;
+  const float *least; // [rows] second pass: T
+  int32_t *found, *count;
+};
+
+// First pass (Find = false) or second.  A wavefront owns 64 rows; the matrix instructions' rate bounds both.
+template <int KC, bool Find>
+__global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
+  constexpr int kStage = kScoreTiles * KC * kFrag, kRowRoom = row_room(KC);
+  __shared__ _Float16 buf[2 * kStage];
+  __shared__ int32_t list[Find ? kWaves * 64 * kRowRoom : 1], have[Find ? kWaves * 64 : 1];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.x % a.splits;
+  const int64_t own_tile = (static_cast<int64_t>(blockIdx.x / a.splits) * kWaves + wave) * 2;
+  const int64_t s0 = split * a.steps_per_split, s1 = min(s0 + a.steps_per_split, a.steps);
+  auto fetch = [&](int64_t step, int at) {
+    const _Float16 *src = a.str + step * kStage;
+    const int n = static_cast<int>(min(static_cast<int64_t>(kScoreTiles), a.tiles - step * kScoreTiles)) * KC;
+    for (int f = wave; f < n; f += kWaves)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src + f * kFrag + lane * 8)),
+                                       (__attribute__((address_space(3))) uint32_t *)(buf + at * kStage + f * kFrag), 16, 0, 0);
+  };
+  h8 q[KC][2];
+  int64_t row[2];
+  float least[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const bool live = own_tile + u < a.own_tiles;
+    const _Float16 *own = a.own + (own_tile + u) * (KC + 1) * kFrag;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      q[c][u] = h8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (live) q[c][u] = *reinterpret_cast<const h8 *>(own + (!Find && c == a.last ? KC : c) * kFrag + lane * 8);
+    }
+    row[u] = (own_tile + u) * kTile + (lane & 31);
+    if (row[u] >= a.rows) row[u] = -1;
+    least[u] = __builtin_inff();
+    if (Find && row[u] >= 0) least[u] = a.least[row[u]];
+  }
+  if constexpr (Find) {
+    have[threadIdx.x] = 0;
+  }
+  if (s0 < s1) fetch(s0, 0);
+  for (int64_t st = s0; st < s1; ++st) {
+    const int at = static_cast<int>(st - s0) & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (st + 1 < s1) fetch(st + 1, at ^ 1);
+    float most[2][kScoreTiles];
+#pragma unroll
+    for (int z = 0; z < kScoreTiles; ++z) {
+      const int64_t t = st * kScoreTiles + z;
+      most[0][z] = most[1][z] = -__builtin_inff();
+      if (t >= a.tiles) continue;
+      uint32_t out[2] = {0u, 0u};
+      if (a.excluded) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (row[u] >= 0) out[u] = a.excluded[row[u] * a.words + t] >> (4 * half);
+      }
+      f32x16 s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+      const _Float16 *f = buf + at * kStage + z * KC * kFrag + lane * 8;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const h8 h = *reinterpret_cast<const h8 *>(f + c * kFrag);
+        s[0] = mfma(h, q[c][0], s[0]);
+        s[1] = mfma(h, q[c][1], s[1]);
+      }
+      const bool part = (t + 1) * kTile > a.items;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (!Find) {
+          if (a.excluded) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int bit = 8 * (r >> 2) + (r & 3);
+              if ((out[u] >> bit) & 1) s[u][r] = -__builtin_inff();
+            }
+          }
+          if (part) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.items) s[u][r] = -__builtin_inff();
+          }
+          float m = s[u][0];
+#pragma unroll
+          for (int r = 1; r < 16; ++r) m = fmaxf(m, s[u][r]);
+          most[u][z] = m;
+        } else {
+          uint32_t hits = 0;
+#pragma unroll
+          for (int r = 15; r >= 0; --r) hits = hits * 2 + (s[u][r] < least[u] ? 0u : 1u);  // NaN is a candidate
+          if (row[u] < 0) hits = 0;
+          if (__any(hits != 0)) {
+            // the excluded, and in the last tile what lies behind the items
+            hits &= ~((out[u] & 15) | ((out[u] >> 4) & 0xf0) | ((out[u] >> 8) & 0xf00) | ((out[u] >> 12) & 0xf000));
+            if (part)
+              for (int r = 0; r < 16; ++r)
+                if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.items) hits &= ~(1u << r);
+            if (hits) {
+              const int mine = wave * 64 + u * 32 + (lane & 31);
+              int to = atomicAdd(&have[mine], __popc(hits));
+              while (hits) {
+                const int r = __ffs(hits) - 1;
+                hits &= hits - 1;
+                const int32_t j = static_cast<int32_t>(t * kTile) + 8 * (r >> 2) + 4 * half + (r & 3);
+                if (to < kRowRoom) {
+                  list[mine * kRowRoom + to] = j;
+                } else {
+                  const int g = atomicAdd(&a.count[row[u]], 1);
+                  if (g < kCandidates) a.found[row[u] * kCandidates + g] = j;
+                }
+                ++to;
+              }
+            }
+          }
+        }
+      }
+    }
+    if constexpr (!Find) {
+      static_assert(kScoreTiles == 2, "stored as pairs");
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (row[u] >= 0)
+          *reinterpret_cast<float2 *>(a.most + (row[u] * a.steps + st) * 4 + half * 2) = make_float2(most[u][0], most[u][1]);
+    }
+  }
+  if constexpr (Find) {
+    __syncthreads();
+    for (int m = wave * 64; m < wave * 64 + 64; ++m) {  // a row's list to the others' of its row
+      const int64_t r = own_tile * kTile + (m & 63);
+      const int n = min(have[m], kRowRoom);
+      if (r >= a.rows || n == 0) continue;
+      int to = 0;
+      if (lane == 0) to = atomicAdd(&a.count[r], n);
+      to = __shfl(to, 0);
+      if (lane < n && to + lane < kCandidates) a.found[r * kCandidates + to + lane] = list[m * kRowRoom + lane];
+    }
+  }
+}
+
+__device__ inline uint32_t order_bits(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+__device__ inline float bits_value(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
+
+// T of each row: the k-th largest of its bounds, rounded down to the upper 22 bits (two histograms of 11 bits).  One
+// workgroup per row; bound by the reads of the bounds.
+__global__ __launch_bounds__(kThreads) void k_top_least(const float *most, int64_t per_row, int32_t k, float *least) {
+  __shared__ int32_t hist[2048], sh[4], digit, left;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float *row = most + blockIdx.x * per_row;
+  uint32_t prefix = 0;
+  int need = k;
+  for (int round = 0; round < 2; ++round) {
+    const int shift = round ? 10 : 21;
+    for (int b = threadIdx.x; b < 2048; b += kThreads) hist[b] = 0;
+    __syncthreads();
+    for (int64_t q = threadIdx.x; q < per_row; q += kThreads) {
+      const uint32_t u = order_bits(row[q]);
+      if (round == 0 || u >> 21 == prefix) atomicAdd(&hist[(u >> shift) & 2047], 1);
+    }
+    __syncthreads();
+    // digits from the largest down: thread i holds 2047 - 8i .. 2040 - 8i
+    int own = 0;
+    for (int z = 0; z < 8; ++z) own += hist[2047 - 8 * threadIdx.x - z];
+    int s = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(s, o);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) sh[wave] = s;
+    if (threadIdx.x == 0) digit = -1;
+    __syncthreads();
+    int above = s - own;
+    for (int w = 0; w < wave; ++w) above += sh[w];
+    if (above < need && above + own >= need) {
+      for (int z = 0; z < 8; ++z) {
+        const int b = 2047 - 8 * threadIdx.x - z;
+        if (above + hist[b] >= need) {
+          digit = b;
+          left = need - above;
+          break;
+        }
+        above += hist[b];
+      }
+    }
+    __syncthreads();
+    if (digit < 0) {  // fewer than k bounds
+      if (threadIdx.x == 0) least[blockIdx.x] = -__builtin_inff();
+      return;
+    }
+    prefix = round ? prefix << 11 | digit : digit;
+    need = left;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) least[blockIdx.x] = bits_value(prefix << 10);
+}
+
+// The candidates of a row (or all items) in order
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_top_rank(TopArgs<T> a) {
+  __shared__ double x[kMaxK];
+  __shared__ uint64_t keys[kTopRoom];
+  __shared__ int32_t items[kTopRoom], count;
+  const int64_t r = blockIdx.x;
+  const Best b{keys, items, &count};
+  top_row(a, r, x, &count);
+  const int n = a.count[r];
+  if (n > a.room) {
+    top_all(a, r, x, b, 0, a.items);
+  } else {
+    uint64_t least = 0;
+    for (int base = 0; base < n; base += kThreads)
+      top_batch(a, x, b, least, [&](int q) { return base + q < n ? a.found[r * a.room + base + q] : -1; });
+    best_cut(b, a.k);
+  }
+  top_out(a, r, b);
 }
 
 __global__ __launch_bounds__(kThreads) void k_clear(uint32_t *p, int64_t n) {
@@ -1579,28 +1944,78 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
   return PS_SOFT_OK;
 }
 
-// Rows of one launch of the item search: their exclusion bits and pieces' results stay below a gigabyte
+// Chunks of 16 numbers, the bound's among them, that the search's passes are built for
+int32_t score_chunks(int32_t K) {
+  for (int32_t c : {2, 3, 5, 7, 9, 13, 17, 25})
+    if (K + 1 <= 16 * c) return c;
+  return 33;
+}
+
 struct TopPlan {
-  int64_t rows, per;
-  int32_t pieces, words;
-  int64_t bits, key, item, bytes;
+  bool filter;
+  int64_t rows;  // rows of one launch: what they need stays near a gigabyte
+  int64_t per;
+  int32_t pieces, words, kc;
+  int64_t xt, wt, steps, per_split;
+  int32_t splits;
+  int64_t bits, key, item, part, px, pw, most, least, found, count, bytes;
 };
+
 TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
   TopPlan p{};
+  const int64_t all = std::max<int64_t>(n, 1);
   p.words = static_cast<int32_t>(up(h->items, 32));
-  const int64_t rows = std::max<int64_t>(n, 1);
-  p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min({up(512, rows), up(h->items, kThreads), static_cast<int64_t>(256)})));
-  if (h->splits > 0) p.pieces = static_cast<int32_t>(std::min<int64_t>(h->splits, h->items));
-  p.per = up(h->items, p.pieces);
-  p.pieces = static_cast<int32_t>(up(h->items, p.per));
-  const int64_t per_row = (exclude ? p.words * 4LL : 0) + static_cast<int64_t>(p.pieces) * k * 12;
-  p.rows = std::min(rows, std::max<int64_t>(1, (1LL << 30) / per_row));
+  p.filter = all > 32 && h->items > 2048 && h->items < 1 << 30;
   Arena a;
+  if (p.filter) {
+    p.kc = score_chunks(h->K);
+    p.wt = up(h->items, kTile);
+    p.steps = up(p.wt, kScoreTiles);
+    const int64_t per_row = (exclude ? p.words * 4LL : 0) + p.steps * 16 + kCandidates * 4 + (p.kc + 1) * 32;
+    p.rows = std::min(all, std::max<int64_t>(256, (1LL << 30) / per_row / 256 * 256));
+    p.xt = up(p.rows, kTile);
+    p.splits = pieces(up(p.xt, 2), p.steps, h->splits);
+    p.per_split = up(p.steps, p.splits);
+    p.splits = static_cast<int32_t>(up(p.steps, p.per_split));
+    p.part = a.take(2 * kParts * 4);
+    p.px = a.take(p.xt * (p.kc + 1) * kFrag * 2);
+    p.pw = a.take(p.wt * p.kc * kFrag * 2);
+    p.most = a.take(p.rows * p.steps * 16);
+    p.least = a.take(p.rows * 4);
+    p.found = a.take(p.rows * kCandidates * 4);
+    p.count = a.take(p.rows * 4);
+  } else {
+    p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min({up(512, all), up(h->items, kThreads), static_cast<int64_t>(256)})));
+    if (h->splits > 0) p.pieces = static_cast<int32_t>(std::min<int64_t>(h->splits, h->items));
+    p.per = up(h->items, p.pieces);
+    p.pieces = static_cast<int32_t>(up(h->items, p.per));
+    const int64_t per_row = (exclude ? p.words * 4LL : 0) + static_cast<int64_t>(p.pieces) * k * 12;
+    p.rows = std::min(all, std::max<int64_t>(1, (1LL << 30) / per_row));
+    p.key = a.take(p.rows * p.pieces * k * 8);
+    p.item = a.take(p.rows * p.pieces * k * 4);
+  }
   p.bits = a.take(exclude ? p.rows * p.words * 4 : 0);
-  p.key = a.take(p.rows * p.pieces * k * 8);
-  p.item = a.take(p.rows * p.pieces * k * 4);
   p.bytes = a.at;
   return p;
+}
+
+template <int KC, bool Find>
+void run_score_of(const ScoreArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((k_score<KC, Find>), dim3(static_cast<unsigned>(up(a.own_tiles, 2 * kWaves) * a.splits)), dim3(kThreads), 0, s, a);
+}
+template <bool Find>
+void run_score(const ScoreArgs &a, int32_t kc, hipStream_t s) {
+  switch (kc) {
+    case 2: return run_score_of<2, Find>(a, s);
+    case 3: return run_score_of<3, Find>(a, s);
+    case 5: return run_score_of<5, Find>(a, s);
+    case 7: return run_score_of<7, Find>(a, s);
+    case 9: return run_score_of<9, Find>(a, s);
+    case 13: return run_score_of<13, Find>(a, s);
+    case 17: return run_score_of<17, Find>(a, s);
+    case 25: return run_score_of<25, Find>(a, s);
+    default: return run_score_of<33, Find>(a, s);
+  }
 }
 
 template <class T>
@@ -1609,6 +2024,8 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
   const TopPlan p = top_plan(h, n, k, row_ptr != nullptr);
   const int rc = grow(h, p.bytes);
   if (rc) return rc;
+  char *const base = h->work;
+  hipStream_t s = h->stream;
   TopArgs<T> a{};
   a.items = static_cast<int32_t>(h->items);
   a.K = h->K;
@@ -1616,24 +2033,64 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
   a.words = p.words;
   a.x = Table<T>{X, ldx, n, aligned4(X, ldx), nullptr};
   a.w = Table<T>{W, ldw, h->items, aligned4(W, ldw), nullptr};
-  uint32_t *bits = reinterpret_cast<uint32_t *>(h->work + p.bits);
+  uint32_t *bits = reinterpret_cast<uint32_t *>(base + p.bits);
   a.excluded = row_ptr ? bits : nullptr;
   a.per_piece = p.per;
   a.pieces = p.pieces;
-  a.key = reinterpret_cast<uint64_t *>(h->work + p.key);
-  a.item = reinterpret_cast<int32_t *>(h->work + p.item);
+  a.key = reinterpret_cast<uint64_t *>(base + p.key);
+  a.item = reinterpret_cast<int32_t *>(base + p.item);
+  a.found = reinterpret_cast<int32_t *>(base + p.found);
+  a.count = reinterpret_cast<int32_t *>(base + p.count);
+  a.room = kCandidates;
   a.out_item = top_item;
   a.out_score = top_score;
   a.ldo = ldo;
+  float *part = reinterpret_cast<float *>(base + p.part);
+  if (p.filter && h->type != PS_SOFT_F16)
+    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kThreads), 0, s, a.x, a.w, h->K, part);
   for (a.row0 = 0; a.row0 < n; a.row0 += p.rows) {
     a.n = std::min(p.rows, n - a.row0);
+    const unsigned rows = static_cast<unsigned>(a.n);
     if (row_ptr) {
-      hipLaunchKernelGGL(k_clear, dim3(blocks_for(a.n * p.words, kThreads * 4, 8192)), dim3(kThreads), 0, h->stream, bits, a.n * p.words);
-      hipLaunchKernelGGL(k_exclude, dim3(static_cast<unsigned>(up(a.n, 4))), dim3(kThreads), 0, h->stream, row_ptr, item, entries, a.row0,
+      hipLaunchKernelGGL(k_clear, dim3(blocks_for(a.n * p.words, kThreads * 4, 8192)), dim3(kThreads), 0, s, bits, a.n * p.words);
+      hipLaunchKernelGGL(k_exclude, dim3(static_cast<unsigned>(up(a.n, 4))), dim3(kThreads), 0, s, row_ptr, item, entries, a.row0,
                          a.n, a.items, p.words, bits);
     }
-    hipLaunchKernelGGL((k_top_scan<T>), dim3(static_cast<unsigned>(a.n), static_cast<unsigned>(p.pieces)), dim3(kThreads), 0, h->stream, a);
-    hipLaunchKernelGGL((k_top_join<T>), dim3(static_cast<unsigned>(a.n)), dim3(kThreads), 0, h->stream, a);
+    if (!p.filter) {
+      hipLaunchKernelGGL((k_top_scan<T>), dim3(rows, static_cast<unsigned>(p.pieces)), dim3(kThreads), 0, s, a);
+      if (p.pieces > 1) hipLaunchKernelGGL((k_top_join<T>), dim3(rows), dim3(kThreads), 0, s, a);
+      continue;
+    }
+    ScoreArgs q{};
+    _Float16 *px = reinterpret_cast<_Float16 *>(base + p.px), *pw = reinterpret_cast<_Float16 *>(base + p.pw);
+    int32_t *count = reinterpret_cast<int32_t *>(base + p.count);
+    const int64_t xt = up(a.n, kTile);
+    const float c = (h->type == PS_SOFT_F32 ? 0x1p-10f + 0x1p-22f : 0.f) + (2 * p.kc + 16) * 0x1p-22f + std::sqrt(static_cast<float>(h->K)) * 0x1p-24f;
+    const int kd = std::min((h->K + 31) / 32, kPackBlocks);
+    hipLaunchKernelGGL((k_top_pack<T>), dim3(static_cast<unsigned>(xt + (a.row0 ? 0 : p.wt))), dim3(kThreads),
+                       static_cast<unsigned>(kTile * (kd * 32 + 1) * 4), s, a.x, a.w, a.row0, a.n, static_cast<int32_t>(xt), px, pw, h->K,
+                       p.kc, c, part, count);
+    q.own = px;
+    q.str = pw;
+    q.rows = a.n;
+    q.own_tiles = xt;
+    q.tiles = p.wt;
+    q.steps_per_split = p.per_split;
+    q.items = a.items;
+    q.splits = p.splits;
+    q.words = p.words;
+    q.last = h->K / 16;
+    q.excluded = a.excluded;
+    q.most = reinterpret_cast<float *>(base + p.most);
+    q.steps = p.steps;
+    float *least = reinterpret_cast<float *>(base + p.least);
+    q.least = least;
+    q.found = reinterpret_cast<int32_t *>(base + p.found);
+    q.count = count;
+    run_score<false>(q, p.kc, s);
+    hipLaunchKernelGGL(k_top_least, dim3(rows), dim3(kThreads), 0, s, q.most, p.steps * 4, k, least);
+    run_score<true>(q, p.kc, s);
+    hipLaunchKernelGGL((k_top_rank<T>), dim3(rows), dim3(kThreads), 0, s, a);
   }
   SOFT_TRY(h, hipGetLastError());
   return PS_SOFT_OK;

@@ -237,6 +237,59 @@ def test_top(soft, n, M, K, k, mean, splits, dtype):
     assert np.all(np.abs(a[fine] - b[fine]) <= 2 * soft_ref.U * np.abs(b[fine]) + 1e-30)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,M,K,k,mean,splits", [(33, 2049, 1, 3, 0, 0), (40, 2100, 15, 256, 30, 0), (65, 3000, 16, 10, 20, 3), (257, 2500, 31, 64, 0, 0),
+                                                 (300, 4100, 100, 33, 500, 0), (130, 9000, 128, 100, 0, 5), (50, 2600, 200, 20, 10, 0),
+                                                 (64, 2300, 256, 7, 0, 0), (34, 2400, 300, 40, 9, 0), (90, 2222, 512, 12, 0, 0),
+                                                 (1000, 20_011, 40, 50, 100, 0)])
+def test_top_of_many_rows(soft, n, M, K, k, mean, splits, dtype):
+    # enough rows and items for the search by candidates
+    test_top(soft, n, M, K, k, mean, splits, dtype)
+
+
+def test_top_of_uneven_tables(soft):
+    # rows and items of far lengths, a few items above all, near scores, rows of zeros or not finite, many equal items
+    g = gen(21)
+    n, M, K, k = 100, 5000, 48, 30
+    X, W = tables(n, M, K, F32, g)
+    W *= torch.exp(1.5 * torch.randn(M, 1, generator=g)).cuda()
+    X *= torch.exp2(torch.randint(-40, 20, (n, 1), generator=g).float()).cuda()
+    W[100:140] *= 300
+    W[2000:2600] = W[1999]  # 601 equal items
+    W[3000:4500] = W[1999] + 1e-6 * torch.randn(1500, K, generator=g).cuda()  # and 1500 near ones
+    X[:50] = W[1999] * X[:50].norm(dim=1, keepdim=True)  # half of the rows like them best
+    X[60] = 0
+    ptr = torch.zeros(n + 1, dtype=torch.int64)
+    ptr[3:] = 4990  # row 2 leaves ten
+    ptr[11:] += 40  # row 10 excludes the longest
+    item = torch.cat((torch.arange(4990), torch.arange(100, 140))).int().cuda()
+    for name, w in (("finite", W), ("nan", W.clone()), ("inf", W.clone())):
+        if name != "finite":
+            w[777, 5] = float(name)
+        want, score = soft_ref.top(X, w, k, ptr, item)
+        say(f"top uneven {name}")
+        with soft.PsSoft(M, K) as h:
+            best, val = h.top(X, w, k, row_ptr=ptr.cuda(), item=item)
+        got = best.cpu().numpy()
+        if name == "finite":
+            # equal up to the order of scores whose 64-bit sums differ in their last bits
+            s = soft_ref.f64(X) @ soft_ref.f64(w).T
+            for i in range(n):
+                if not np.array_equal(got[i], want[i]):
+                    a, b = s[i, got[i]], s[i, want[i]]
+                    assert (got[i] >= 0).all() and np.abs(a - b).max() <= 64 * 2.0 ** -53 * np.abs(s[i]).max(), i
+                    assert len(set(got[i])) == k
+            assert (got[2, 10:] == -1).all() and (got[60] == np.arange(k)).all()
+        else:
+            rows = [i for i in range(n) if i != 2]
+            s = soft_ref.f64(X) @ soft_ref.f64(w).T
+            for i in rows:
+                if np.isnan(s[i, 777]) or s[i, 777] == np.inf:
+                    assert got[i, 0] == 777, (name, i)
+                else:
+                    assert 777 not in got[i]
+
+
 def test_top_ties_masks_and_nan(soft):
     # whole numbers: many equal scores, exact in any order; the lowest items win
     g = gen(6)
