@@ -393,6 +393,20 @@ struct PassArgs {
 
 __device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
+// Scheduling of a run of steps, each R reads of fragments from LDS and M matrix instructions: reads go ahead of their use
+// by about 6 matrix instructions (192 cycles).  Left to the compiler, each step waited for its own reads
+template <int Steps, int R, int M>
+__device__ inline void order_reads() {
+  constexpr int ahead = (5 + M) / M < Steps ? (5 + M) / M : Steps;
+  __builtin_amdgcn_sched_group_barrier(0x100, ahead * R, 0);
+#pragma unroll
+  for (int c = 0; c < Steps - ahead; ++c) {
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, ahead * M, 0);
+}
+
 constexpr int kLds = 160 * 1024;
 constexpr int kHalfTile = kTile * 16;  // floats of half a tile's targets
 constexpr int kWaves = 4;  // wavefronts of a pass's workgroup: 128 own rows
@@ -553,6 +567,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
         s = mfma(l, q[c][0], s);
       }
     }
+    order_reads<KC, NP, NP == 2 ? 3 : 1>();
     // log2 weights: the score's, less the row's log-sum-exp where it is known.  That is subtracted here: as the
     // matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
     float p[16], share[16];
@@ -611,10 +626,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       sum = now;
     }
     if constexpr (DB > 0) {
-      const _Float16 *turned = st + sg.scores * kFrag + lane * 8;
+      if (COL && targets) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (COL && targets) {
+        for (int k = 0; k < 2; ++k) {
           // this half tile's records, through the wavefront's own table of 32 items x 16 rows in LDS, zero between uses.  A
           // row that lists an item twice adds twice: one wavefront's LDS additions come in the order of its
           // instructions and, within one, in an order that its addresses alone decide.
@@ -649,6 +663,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
             }
           }
         }
+      }
+      const _Float16 *turned = st + sg.scores * kFrag + lane * 8;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
         // a weight and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
         // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
 #pragma unroll
@@ -668,6 +686,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           if constexpr (NP == 2) o[b] = mfma(*reinterpret_cast<const h8 *>(f + kFrag), ph, o[b]);
         }
       }
+      order_reads<2 * DB, NP, NP + 1>();
     }
   }
   if (!live) return;
