@@ -381,7 +381,7 @@ struct PassArgs {
   int64_t own_stride, str_stride;  // halves per tile
   int64_t own_tiles, str_rows;
   int32_t d0;                      // the first block of 32 numbers summed here
-  int32_t splits, buffers;         // pieces of the stream; tiles in LDS
+  int32_t splits;                  // pieces of the stream
   const float *rowvec;             // COL: per tile of 32 stream rows, 32 times minus the log2-sum-exp, and 32 shares
   const Scal *scal;
   float scale;                     // log2(e) / tau
@@ -393,33 +393,63 @@ struct PassArgs {
 
 __device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-// Scheduling of a run of steps, each R reads of fragments from LDS and M matrix instructions: reads go ahead of their use
-// by about 6 matrix instructions (192 cycles).  Left to the compiler, each step waited for its own reads
-template <int Steps, int R, int M>
-__device__ inline void order_reads() {
-  constexpr int ahead = (5 + M) / M < Steps ? (5 + M) / M : Steps;
-  __builtin_amdgcn_sched_group_barrier(0x100, ahead * R, 0);
-#pragma unroll
-  for (int c = 0; c < Steps - ahead; ++c) {
-    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(0x008, ahead * M, 0);
+// From memory to LDS without registers: lane l's 16 (4) bytes at `from` go to `to` + 16 (4) l; `to` is the wavefront's
+typedef const __attribute__((address_space(1))) uint32_t *global_ptr;
+typedef __attribute__((address_space(3))) uint32_t *lds_ptr;
+__device__ inline void to_lds16(const void *from, void *to) {
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<global_ptr>(reinterpret_cast<uintptr_t>(from)), (lds_ptr)to, 16, 0, 0);
 }
+__device__ inline void to_lds4(const void *from, void *to) {
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<global_ptr>(reinterpret_cast<uintptr_t>(from)), (lds_ptr)to, 4, 0, 0);
+}
+
+// The rest of a number behind a half of `h`, p - h (one instruction: the half is read as it is).  On the rounded fp16
+// number itself: a product and its rounding, fused at one of two uses, once gave a rest of another
+// fp16 number (2^-11 off in a weight of a thousand)
+__device__ inline float rest_low(uint32_t h, float p) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+  return r;
+}
+__device__ inline float rest_high(uint32_t h, float p) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+  return r;
+}
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t to_halves(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, h2));
+}
+// Both planes of two weights
+__device__ inline void planes(float a, float b, uint32_t &h, uint32_t &l) {
+  h = to_halves(a, b);
+  l = to_halves(rest_low(h, a), rest_high(h, b));
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ inline h8 halves(u32x4 v) { return __builtin_bit_cast(h8, v); }
 
 constexpr int kLds = 160 * 1024;
 constexpr int kHalfTile = kTile * 16;  // floats of half a tile's targets
 constexpr int kWaves = 4;  // wavefronts of a pass's workgroup: 128 own rows
 
-// Fragments of one tile that a pass stages: k16 NP for the scores, then 2 nb NP turned ones
+// LDS of a pass, in halves: tiles' fragments for the scores (one or two tiles), the turned ones (two), the row values of a
+// pass over rows (four) and its wavefronts' targets
 struct Stage {
-  int scores, turned, halves;  // halves: with the row values of a pass over rows
+  int scores, turned;   // fragments: for the scores, and the turned ones of each half of the tile's rows
+  int score_tiles;      // tiles of score fragments
+  int at_turned, at_rows, at_targets, halves;
 };
-__host__ __device__ constexpr Stage stage_of(int np, int k16, int nb, bool col) {
+__host__ __device__ constexpr Stage stage_of(int np, int kc, int db, bool col) {
   Stage s{};
-  s.scores = k16 * np;
-  s.turned = nb * np;  // of each half of the tile's rows
-  s.halves = (s.scores + 2 * s.turned) * kFrag + (col ? 128 : 0);
+  s.scores = kc * np;
+  s.turned = db * np;
+  const int rest = 2 * 2 * s.turned * kFrag + (col ? 4 * 128 + kWaves * kHalfTile * 2 : 0);
+  s.score_tiles = (2 * s.scores * kFrag + rest) * 2 <= kLds ? 2 : 1;
+  s.at_turned = s.score_tiles * s.scores * kFrag;
+  s.at_rows = s.at_turned + 2 * 2 * s.turned * kFrag;
+  s.at_targets = s.at_rows + (col ? 4 * 128 : 0);
+  s.halves = s.at_turned + rest;
   return s;
 }
 
@@ -471,9 +501,11 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 }
 
 // Rows over items (COL = false) or items over rows (COL = true).  A wavefront owns 32 rows; the stream's tiles go
-// through LDS, shared by the workgroup, the next one loaded while one is used.
+// through LDS, shared by the workgroup, loaded one step ahead of their use.
 // Score instruction: stream rows x own rows, so a lane holds one own row (l%32) and 16 stream rows
 // 8(r/4) + 4h + r%4 of each tile.
+// The matrix instructions bound it (1.1 PFLOP/s of them at K = 128 fp32, the clock near 1.85 GHz), so the loop keeps them
+// fed: the next tile's scores are made beside the exponentials of this one's, the sums beside the rounding.
 template <int NP, int KC, int DB, bool COL>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
@@ -484,27 +516,32 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   const int split = blockIdx.x % a.splits;
   const int64_t own_tile = static_cast<int64_t>(blockIdx.x / a.splits) * kWaves + wave;
   const int64_t tiles = (a.str_rows + kTile - 1) / kTile;
-  const int64_t t0 = split * a.tiles_per_split, t1 = min(t0 + a.tiles_per_split, tiles);
+  const int t0 = static_cast<int>(split * a.tiles_per_split);
+  const int t1 = static_cast<int>(min(t0 + a.tiles_per_split, tiles));
   const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
   const bool live = own_tile < a.own_tiles;  // the last workgroup's wavefronts behind the last row only help loading
-  auto fetch = [&](int64_t t, int at) {
-    const _Float16 *src = a.str + t * a.str_stride;
-    _Float16 *to = buf + at * sg.halves;
+  auto fetch_scores = [&](int t) {
+    const _Float16 *src = a.str + t * a.str_stride + lane * 8;
+    _Float16 *to = buf + (sg.score_tiles == 2 ? (t & 1) * sg.scores * kFrag : 0);
 #pragma unroll
-    for (int f0 = 0; f0 < sg.scores + 2 * sg.turned; f0 += kWaves) {
+    for (int f0 = 0; f0 < sg.scores; f0 += kWaves) {
       const int f = f0 + wave;
-      if ((sg.scores + 2 * sg.turned) % kWaves != 0 && f >= sg.scores + 2 * sg.turned) break;
-      int from = f;
-      if (DB > 0 && DB < KD && f >= sg.scores) {
-        const int g = f - sg.scores, q = g >= sg.turned;
-        from = sg.scores + (q * KD + a.d0) * NP + g - q * sg.turned;
-      }
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src + from * kFrag + lane * 8)),
-                                       (__attribute__((address_space(3))) uint32_t *)(to + f * kFrag), 16, 0, 0);
+      if (sg.scores % kWaves != 0 && f >= sg.scores) break;
+      to_lds16(src + f * kFrag, to + f * kFrag);
     }
-    if (COL && wave == 0)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(a.rowvec + t * 64 + lane)),
-                                       (__attribute__((address_space(3))) uint32_t *)(to + sg.halves - 128), 4, 0, 0);
+  };
+  auto fetch_turned = [&](int t) {
+    const _Float16 *src = a.str + t * a.str_stride + (sg.scores + a.d0 * NP) * kFrag + lane * 8;
+    _Float16 *to = buf + sg.at_turned + (t & 1) * 2 * sg.turned * kFrag;
+#pragma unroll
+    for (int f0 = 0; f0 < 2 * sg.turned; f0 += kWaves) {
+      const int f = f0 + wave;
+      if (2 * sg.turned % kWaves != 0 && f >= 2 * sg.turned) break;
+      to_lds16(src + (f + (f >= sg.turned ? (KD - DB) * NP : 0)) * kFrag, to + f * kFrag);
+    }
+  };
+  auto fetch_rows = [&](int t) {
+    if (COL && wave == 0) to_lds4(a.rowvec + static_cast<int64_t>(t) * 64 + lane, buf + sg.at_rows + (t & 3) * 128);
   };
   h8 q[KC][NP];
   const _Float16 *own = a.own + own_tile * a.own_stride;
@@ -528,75 +565,106 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   Window win;
   float *y = nullptr;
   if constexpr (COL) {
-    y = reinterpret_cast<float *>(buf + a.buffers * sg.halves) + wave * kHalfTile;
+    y = reinterpret_cast<float *>(buf + sg.at_targets) + wave * kHalfTile;
 #pragma unroll
     for (int r = 0; r < kHalfTile / 64; ++r) y[r * 64 + lane] = 0.f;
     if (a.first && live) {
-      const int64_t b = first_of_row(a.pay, a.first[own_tile], a.first[own_tile + 1], static_cast<uint32_t>(t0 * kTile), lane);
+      const int64_t b = first_of_row(a.pay, a.first[own_tile], a.first[own_tile + 1], static_cast<uint32_t>(t0) * kTile, lane);
       const int64_t e = a.first[own_tile + 1];
       win.open(a.pay, b, e, lane);
-      targets = __any(win.now.x >> 5 < static_cast<uint64_t>(t1) * kTile);
+      targets = __any((win.now.x >> 5) < static_cast<uint32_t>(t1) * kTile);
     }
     if (targets) {
       ref = -kLag;
       unit = ldexpf(1.f / a.scal->amax, static_cast<int>(kShift + kLag));
     }
   }
-  int at = 0;
-  if (a.buffers == 2) fetch(t0, 0);
-  for (int64_t t = t0; t < t1; ++t) {
-    if (a.buffers == 1) {
-      __syncthreads();
-      fetch(t, 0);
+  // Chunk c of a tile's score fragments, and step i of its turned ones (half i / DB, block i % DB)
+  auto read_scores = [&](h8 (&f)[NP], int t, int c) {
+    const _Float16 *from = buf + (sg.score_tiles == 2 ? (t & 1) * sg.scores * kFrag : 0) + c * NP * kFrag + lane * 8;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) f[p] = *reinterpret_cast<const h8 *>(from + p * kFrag);
+  };
+  auto read_turned = [&](h8 (&f)[NP], int t, int i) {
+    const _Float16 *from = buf + sg.at_turned + ((t & 1) * 2 * sg.turned + i * NP) * kFrag + lane * 8;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) f[p] = *reinterpret_cast<const h8 *>(from + p * kFrag);
+  };
+  auto add_scores = [&](f32x16 s, const h8 (&f)[NP], int c) {
+    s = mfma(f[0], q[c][0], s);
+    if constexpr (NP == 2) {
+      s = mfma(f[0], q[c][1], s);
+      s = mfma(f[1], q[c][0], s);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (a.buffers == 2 && t + 1 < t1) fetch(t + 1, at ^ 1);
-    const _Float16 *st = buf + at * sg.halves;
-    if (a.buffers == 2) at ^= 1;
+    return s;
+  };
+  // log2 weights of stream rows r: the score's, less the row's log-sum-exp where it is known.  That is subtracted here: as
+  // the matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
+  auto row_values = [&](int t, int g, int which) {  // rows 8g + 4h ..+3: minus the log-sum-exps, or the shares
+    return *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(buf + sg.at_rows + (t & 3) * 128) + which * 32 + g * 8 + half * 4);
+  };
+  fetch_scores(t0);
+  if constexpr (DB > 0) fetch_turned(t0);
+  fetch_rows(t0);
+  if (t0 + 1 < t1) {
+    if (sg.score_tiles == 2) fetch_scores(t0 + 1);
+    fetch_rows(t0 + 1);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  float p[16], top;
+  auto weigh = [&](const f32x16 &s, int t) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 v = COL ? row_values(t, g, 0) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[4 * g + i] = COL ? fmaf(s[4 * g + i], sc, v[i]) : s[4 * g + i] * sc;
+    }
+    top = p[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
+  };
+  {
     f32x16 s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const h8 h = *reinterpret_cast<const h8 *>(st + (c * NP) * kFrag + lane * 8);
-      s = mfma(h, q[c][0], s);
-      if constexpr (NP == 2) {
-        const h8 l = *reinterpret_cast<const h8 *>(st + (c * NP + 1) * kFrag + lane * 8);
-        s = mfma(h, q[c][1], s);
-        s = mfma(l, q[c][0], s);
-      }
+      h8 f[NP];
+      read_scores(f, t0, c);
+      s = add_scores(s, f, c);
     }
-    order_reads<KC, NP, NP == 2 ? 3 : 1>();
-    // log2 weights: the score's, less the row's log-sum-exp where it is known.  That is subtracted here: as the
-    // matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
-    float p[16], share[16];
-    if constexpr (COL) {
-      const float *rv = reinterpret_cast<const float *>(st + sg.halves - 128);
+    weigh(s, t0);
+  }
+  __syncthreads();  // all have read the first tile: the loop's first step loads over it
+  if (sg.score_tiles == 1 && t0 + 1 < t1) {
+    fetch_scores(t0 + 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  // Steps of matrix instructions whose fragments are read ahead, about 6 instructions (192 cycles)
+  constexpr int SA = NP == 2 ? 2 : 4, TA = NP == 2 ? 2 : 3;
+  for (int t = t0; t < t1; ++t) {
+    if (t + 2 < t1) {
+      if (sg.score_tiles == 2) fetch_scores(t + 2);
+      fetch_rows(t + 2);
+    }
+    if (DB > 0 && t + 1 < t1) fetch_turned(t + 1);
+    h8 f[KC + SA][NP];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(rv + g * 8 + half * 4);
-        const f32x4 u = *reinterpret_cast<const f32x4 *>(rv + 32 + g * 8 + half * 4);
+    for (int c = 0; c < SA && c < KC; ++c) read_scores(f[c], t + 1, c);
+    if (!COL && (t + 1) * static_cast<int64_t>(kTile) > a.str_rows) {  // items behind the last
+      const int left = static_cast<int>(a.str_rows - t * static_cast<int64_t>(kTile)) - 4 * half;
+      top = -__builtin_inff();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[g * 4 + i] = fmaf(s[g * 4 + i], sc, v[i]);
-          share[g * 4 + i] = u[i];
-        }
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = s[r] * sc;
-      if ((t + 1) * kTile > a.str_rows) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (t * kTile + 8 * (r >> 2) + 4 * half + (r & 3) >= a.str_rows) p[r] = -__builtin_inff();
+      for (int r = 0; r < 16; ++r) {
+        if (8 * (r >> 2) + (r & 3) >= left) p[r] = -__builtin_inff();
+        top = fmaxf(top, p[r]);
       }
     }
     if (!COL || !targets) {
-      float top = p[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
-      top = fmaxf(top, __shfl_xor(top, 32));
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
       if (__any(top > ref + kLag)) {
         const float to = top > ref + kLag ? top : ref;
         const float down = __builtin_amdgcn_exp2f(ref - to);
@@ -609,21 +677,42 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           for (int r = 0; r < 16; ++r) o[b][r] *= down;
       }
     }
+    const float shift = kShift - ref;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    f32x4 share[4];
+    if constexpr (COL) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      p[r] = __builtin_amdgcn_exp2f(p[r] + (kShift - ref));
-      if constexpr (COL) p[r] *= share[r];
+      for (int g = 0; g < 4; ++g) share[g] = row_values(t, g, 1);
+    }
+    // the next tile's scores beside this one's weights (behind the last tile: what lies in LDS, and not used)
+    f32x16 next;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) next[r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      if (c + SA < KC) read_scores(f[c + SA], t + 1, c + SA);
+      next = add_scores(next, f[c], c);
+#pragma unroll
+      for (int r = 16 * c / KC; r < 16 * (c + 1) / KC; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(p[r] + shift);
+        if constexpr (COL) p[r] *= share[r >> 2][r & 3];
+        else w[r & 3] += p[r];
+        asm volatile("" : "+v"(p[r]));  // here, beside the matrix instructions
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!COL) {
       // the tile's sum first, and what each addition loses kept: one by one, thousands of small weights were rounded
       // away against the sum (6e-6 of it over 17,770 items)
-      float w[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) w[r] = p[r] + p[r + 8];
-      const float add = (((w[0] + w[4]) + (w[1] + w[5])) + ((w[2] + w[6]) + (w[3] + w[7]))) - lost;
+      const float add = ((w[0] + w[1]) + (w[2] + w[3])) - lost;
       const float now = sum + add;
       lost = (now - sum) - add;
       sum = now;
+    }
+    if (sg.score_tiles == 1 && t + 2 < t1) {
+      __syncthreads();
+      fetch_scores(t + 2);
     }
     if constexpr (DB > 0) {
       if (COL && targets) {
@@ -664,30 +753,52 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           }
         }
       }
-      const _Float16 *turned = st + sg.scores * kFrag + lane * 8;
+      // the sums beside the next tile's log2 weights
+      h8 g[2 * DB + TA][NP];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        // a weight and its rounding to fp16 must not be fused at one of the two uses below: the second plane would be the
-        // rest of another fp16 value than the first's (seen: 2^-11 off in one weight of a thousand)
+      for (int i = 0; i < TA && i < 2 * DB; ++i) read_turned(g[i], t, i);
+      u32x4 ph[2], pl[2];
+      auto make_planes = [&](int k, int i) {
+        uint32_t h, l;
+        planes(p[8 * k + 2 * i], p[8 * k + 2 * i + 1], h, l);
+        ph[k][i] = h;
+        pl[k][i] = l;
+      };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) asm("" : "+v"(p[8 * k + i]));
-        h8 ph, pl;
+      for (int i = 0; i < 4; ++i) make_planes(0, i);
+      float n[16], m[2] = {-__builtin_inff(), -__builtin_inff()};
+      f32x4 v[4];
+      if constexpr (COL) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          ph[i] = static_cast<_Float16>(p[8 * k + i]);
-          pl[i] = static_cast<_Float16>(fmaf(static_cast<float>(ph[i]), -1.f, p[8 * k + i]));
-        }
-#pragma unroll
-        for (int b = 0; b < DB; ++b) {
-          const _Float16 *f = turned + (k * sg.turned + b * NP) * kFrag;
-          const h8 h = *reinterpret_cast<const h8 *>(f);
-          o[b] = mfma(h, ph, o[b]);
-          o[b] = mfma(h, pl, o[b]);
-          if constexpr (NP == 2) o[b] = mfma(*reinterpret_cast<const h8 *>(f + kFrag), ph, o[b]);
-        }
+        for (int z = 0; z < 4; ++z) v[z] = row_values(t + 1, z, 0);
       }
-      order_reads<2 * DB, NP, NP + 1>();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2 * DB; ++i) {
+        const int k = i / DB, b = i % DB;
+        if (i + TA < 2 * DB) read_turned(g[i + TA], t, i + TA);
+        o[b] = mfma(g[i][0], halves(ph[k]), o[b]);
+        o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
+        if constexpr (NP == 2) o[b] = mfma(g[i][1], halves(ph[k]), o[b]);
+        if (k == 0) {
+#pragma unroll
+          for (int z = 4 * b / DB; z < 4 * (b + 1) / DB; ++z) make_planes(1, z);
+        }
+#pragma unroll
+        for (int r = 16 * i / (2 * DB); r < 16 * (i + 1) / (2 * DB); ++r) {
+          n[r] = COL ? fmaf(next[r], sc, v[r >> 2][r & 3]) : next[r] * sc;
+          m[r & 1] = fmaxf(m[r & 1], n[r]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = n[r];
+      top = fmaxf(m[0], m[1]);
+    } else {
+      weigh(next, t + 1);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
   }
   if (!live) return;
   const int64_t row = split * (a.own_tiles * kTile) + own_tile * kTile + (lane & 31);
@@ -1343,8 +1454,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
     const _Float16 *src = a.str + step * kStage;
     const int n = static_cast<int>(min(static_cast<int64_t>(kScoreTiles), a.tiles - step * kScoreTiles)) * KC;
     for (int f = wave; f < n; f += kWaves)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src + f * kFrag + lane * 8)),
-                                       (__attribute__((address_space(3))) uint32_t *)(buf + at * kStage + f * kFrag), 16, 0, 0);
+      to_lds16(src + f * kFrag + lane * 8, buf + at * kStage + f * kFrag);
   };
   h8 q[KC][2];
   int64_t row[2];
@@ -1782,11 +1892,9 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
 }
 
 template <int NP, int KC, int DB>
-void launch_pass(PassArgs a, bool col, hipStream_t s) {
+void launch_pass(const PassArgs &a, bool col, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(up(a.own_tiles, kWaves) * a.splits));
-  const int bytes = stage_of(NP, KC, DB, col).halves * 2;
-  a.buffers = 2 * bytes + (col ? kWaves * kHalfTile * 4 : 0) <= kLds ? 2 : 1;
-  const unsigned lds = static_cast<unsigned>(a.buffers * bytes + (col ? kWaves * kHalfTile * 4 : 0));
+  const unsigned lds = static_cast<unsigned>(stage_of(NP, KC, DB, col).halves * 2);
   if (col) {
     if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64 * kWaves), lds, s, a);
   } else {
