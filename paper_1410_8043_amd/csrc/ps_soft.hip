@@ -453,29 +453,28 @@ __host__ __device__ constexpr Stage stage_of(int np, int kc, int db, bool col) {
   return s;
 }
 
-// The sorted target records of one own tile, in windows of 64, one per lane, three windows read ahead
+// The sorted target records of one own tile, in windows of 64, one per lane, two windows read ahead
 struct Window {
   const uint2 *pay;
-  int64_t base, end;
-  uint2 now, next[3];
-  int pos;
+  int at, end, pos;
+  uint2 now, next[2];
   // a record behind the last: a row above all
-  __device__ uint2 get(int64_t at) const { return at < end ? pay[at] : make_uint2(0xffffffffu, 0u); }
+  __device__ uint2 get(int i) const { return i < end ? pay[i] : make_uint2(0xffffffffu, 0u); }
   __device__ void open(const uint2 *p, int64_t b, int64_t e, int lane) {
-    pay = p;
-    base = b + lane;
-    end = e;
+    pay = p + b;
+    at = lane;
+    end = static_cast<int>(e - b);
     pos = 0;
-    now = get(base);
-    for (int q = 0; q < 3; ++q) next[q] = get(base + 64 * (q + 1));
+    now = get(at);
+    next[0] = get(at + 64);
+    next[1] = get(at + 128);
   }
   __device__ void step() {
-    base += 64;
+    at += 64;
     pos = 0;
     now = next[0];
     next[0] = next[1];
-    next[1] = next[2];
-    next[2] = get(base + 192);
+    next[1] = get(at + 128);
   }
 };
 
@@ -496,8 +495,8 @@ __device__ inline int64_t first_of_row(const uint2 *pay, int64_t b, int64_t e, u
 
 // Wavefronts per SIMD that the registers are cut for
 constexpr int waves_per_simd(int np, int kc, int db) {
-  const int need = 4 * kc * np + 16 * db + 100;  // own rows, sums, and a tile's scores, weights and fragments
-  return need <= 168 ? 3 : need <= 264 ? 2 : 1;
+  const int need = 4 * kc * np + 16 * db;  // own rows and sums; a tile's scores, weights and fragments take 60 to 110 more
+  return need <= 64 ? 3 : need <= 192 && np * kc < 24 ? 2 : 1;
 }
 
 // Rows over items (COL = false) or items over rows (COL = true).  A wavefront owns 32 rows; the stream's tiles go
@@ -643,7 +642,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
     __syncthreads();
   }
   // Steps of matrix instructions whose fragments are read ahead, about 6 instructions (192 cycles)
-  constexpr int SA = NP == 2 ? 2 : 4, TA = NP == 2 ? 2 : 3;
+  // (fewer where 256 numbers of one plane leave no registers)
+  constexpr int SA = NP == 2 || KC >= 16 ? 2 : 4, TA = NP == 2 || KC >= 16 ? 2 : 3;
   for (int t = t0; t < t1; ++t) {
     if (t + 2 < t1) {
       if (sg.score_tiles == 2) fetch_scores(t + 2);
@@ -679,11 +679,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
     }
     const float shift = kShift - ref;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
-    f32x4 share[4];
-    if constexpr (COL) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g) share[g] = row_values(t, g, 1);
-    }
+    f32x4 share[4];  // each read a step ahead of its use
+    if constexpr (COL) share[0] = row_values(t, 0, 1);
     // the next tile's scores beside this one's weights (behind the last tile: what lies in LDS, and not used)
     f32x16 next;
 #pragma unroll
@@ -692,6 +689,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       if (c + SA < KC) read_scores(f[c + SA], t + 1, c + SA);
+      if constexpr (COL) {
+#pragma unroll
+        for (int g = 4 * c / KC + 1; g <= 4 * (c + 1) / KC && g < 4; ++g) share[g] = row_values(t, g, 1);
+      }
       next = add_scores(next, f[c], c);
 #pragma unroll
       for (int r = 16 * c / KC; r < 16 * (c + 1) / KC; ++r) {
@@ -768,15 +769,16 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       for (int i = 0; i < 4; ++i) make_planes(0, i);
       float n[16], m[2] = {-__builtin_inff(), -__builtin_inff()};
       f32x4 v[4];
-      if constexpr (COL) {
-#pragma unroll
-        for (int z = 0; z < 4; ++z) v[z] = row_values(t + 1, z, 0);
-      }
+      if constexpr (COL) v[0] = row_values(t + 1, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < 2 * DB; ++i) {
         const int k = i / DB, b = i % DB;
         if (i + TA < 2 * DB) read_turned(g[i + TA], t, i + TA);
+        if constexpr (COL) {
+#pragma unroll
+          for (int z = 2 * i / DB + 1; z <= 2 * (i + 1) / DB && z < 4; ++z) v[z] = row_values(t + 1, z, 0);
+        }
         o[b] = mfma(g[i][0], halves(ph[k]), o[b]);
         o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
         if constexpr (NP == 2) o[b] = mfma(g[i][1], halves(ph[k]), o[b]);
