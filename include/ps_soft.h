@@ -70,6 +70,9 @@ typedef struct ps_soft ps_soft_t;
 #define PS_SOFT_OPT_SPLITS 2 /* pieces that the reduced axis (items for rows, rows for items) is cut
                                 into, in [1, 1024]; 0 (default): by the sizes.  Sums are joined in a
                                 fixed order; other pieces round otherwise */
+#define PS_SOFT_OPT_SEARCH 3 /* how ps_soft_top searches: 0 all scores in 64 bits; 1 candidates by matrix
+                                instructions first (below 2^30 items); -1 (default): the form estimated
+                                faster.  Same results, bit for bit */
 
 /*
  * Create a handle for tables of `items` items of K numbers of type `type`.  No device memory

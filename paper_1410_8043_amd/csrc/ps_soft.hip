@@ -260,28 +260,38 @@ struct Table {
   const int32_t *act;  // rows that are read (NULL: all)
 };
 
-// Largest finite magnitude of each table, kParts partial maxima each
+// Largest finite magnitude of each table, kParts partial maxima each.  A row's numbers by as many lanes as its float4s,
+// rounded up to a power of two; bound by memory (51 MB at 4.4 TB/s; with a division per float4 it was 0.9).
+constexpr int kScanThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_absmax(Table<T> x, Table<T> w, int32_t K, float *part) {
-  __shared__ float sh[4];
+__global__ __launch_bounds__(kScanThreads) void k_absmax(Table<T> x, Table<T> w, int32_t K, int32_t lanes, float *part) {
+  __shared__ float sh[kScanThreads / 64];
   const bool second = blockIdx.x >= kParts;
   const Table<T> t = second ? w : x;
   const int blk = blockIdx.x - (second ? kParts : 0);
-  const int per = (K + 3) / 4;  // threads per row
+  const int k0 = (threadIdx.x & (lanes - 1)) * 4, rows = kScanThreads / lanes;
+  const int64_t step = static_cast<int64_t>(kParts) * rows;
+  const float inf = __builtin_inff();
   float most = 0.f;
-  const int64_t all = t.rows * per;
-  for (int64_t q = static_cast<int64_t>(blk) * kThreads + threadIdx.x; q < all; q += static_cast<int64_t>(kParts) * kThreads) {
-    const int64_t r = q / per;
-    if (t.act && !t.act[r]) continue;
-    const f32x4 v = load4(t.p + r * t.ld, static_cast<int>(q - r * per) * 4, K, t.vec);
+  if (k0 < K) {
+#pragma unroll 4
+    for (int64_t r = static_cast<int64_t>(blk) * rows + threadIdx.x / lanes; r < t.rows; r += step) {
+      if (t.act && !t.act[r]) continue;
+      const f32x4 v = load4(t.p + r * t.ld, k0, K, t.vec);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float m = fabsf(v[c]);
-      most = fmaxf(most, m < __builtin_inff() ? m : 0.f);
+      for (int c = 0; c < 4; ++c) {
+        const float m = fabsf(v[c]);
+        most = fmaxf(most, m < inf ? m : 0.f);
+      }
     }
   }
-  most = block_max(most, sh);
-  if (threadIdx.x == 0) part[blockIdx.x] = most;
+  most = wave_max(most);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = most;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    most = wave_max(threadIdx.x < kScanThreads / 64 ? sh[threadIdx.x] : 0.f);
+    if (threadIdx.x == 0) part[blockIdx.x] = most;
+  }
 }
 
 __device__ inline int scale_exp(float most) {
@@ -1038,22 +1048,34 @@ struct Records {
   int32_t *key;
   uint2 *pay;
 };
-// first: where the digits start, for the one pass whose digits are the whole keys (NULL otherwise)
+// first: where the digits start, for the one pass whose digits are the whole keys (NULL otherwise).  A lane's 16 keys and
+// payloads are read at once: in turn, each round waited for its own (24 us for 4096 records a workgroup, however few)
 __global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out, int64_t n, int shift, int bits, const int32_t *hist,
                                                         int32_t blocks, const int32_t *total, int64_t *first, int32_t firsts) {
+  constexpr int kOwn = kSortTile / kThreads;
   __shared__ int32_t cnt[4][kBins], sh[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << bits;
-  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / 4);
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / 4) + lane;
+  int32_t key[kOwn];
+  uint2 pay[kOwn];
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q) key[q] = base + 64 * q < n ? in.key[base + 64 * q] : -1;  // keys are not negative
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q) pay[q] = base + 64 * q < n ? in.pay[base + 64 * q] : make_uint2(0u, 0u);
   for (int b = threadIdx.x; b < 4 * kBins; b += kThreads) (&cnt[0][0])[b] = 0;
   __syncthreads();
-#pragma unroll 4
-  for (int q = lane; q < kSortTile / 4; q += 64)
-    if (base + q < n) atomicAdd(&cnt[wave][(in.key[base + q] >> shift) & (bins - 1)], 1);
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q)
+    if (key[q] >= 0) atomicAdd(&cnt[wave][(key[q] >> shift) & (bins - 1)], 1);
   // where each digit starts: the digits before it, four per thread
   const int b0 = 4 * threadIdx.x;
-  int32_t v[4], s = 0;
+  int32_t v[4], at[4], s = 0;
 #pragma unroll
-  for (int z = 0; z < 4; ++z) s += v[z] = b0 + z < bins ? total[b0 + z] : 0;
+  for (int z = 0; z < 4; ++z) {
+    v[z] = b0 + z < bins ? total[b0 + z] : 0;
+    at[z] = b0 + z < bins ? hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x] : 0;
+    s += v[z];
+  }
   const int32_t own = s;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -1068,34 +1090,35 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out,
   for (int z = 0; z < 4; ++z) {
     if (b0 + z < bins) {
       if (first && blockIdx.x == 0 && b0 + z < firsts) first[b0 + z] = before;
-      int32_t at = before + hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x];
+      int32_t to = before + at[z];
+#pragma unroll
       for (int w = 0; w < 4; ++w) {
         const int32_t c = cnt[w][b0 + z];
-        cnt[w][b0 + z] = at;
-        at += c;
+        cnt[w][b0 + z] = to;
+        to += c;
       }
     }
     before += v[z];
   }
   __syncthreads();
   volatile int32_t *mine = cnt[wave];
-  for (int q = lane; q < kSortTile / 4; q += 64) {
-    const bool in_range = base + q < n;
-    const int32_t key = in_range ? in.key[base + q] : 0;
-    const int d = (key >> shift) & (bins - 1);
-    unsigned long long same = __ballot(in_range);
+#pragma unroll
+  for (int q = 0; q < kOwn; ++q) {
+    const bool there = key[q] >= 0;
+    const int d = (key[q] >> shift) & (bins - 1);
+    unsigned long long same = __ballot(there);
     for (int bit = 0; bit < bits; ++bit) {
       const unsigned long long set = __ballot((d >> bit) & 1);
       same &= (d >> bit) & 1 ? set : ~set;
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
-    if (in_range) {
+    if (there) {
       const int32_t to = mine[d] + rank;
-      if (!first) out.key[to] = key;
-      out.pay[to] = in.pay[base + q];
+      if (!first) out.key[to] = key[q];
+      out.pay[to] = pay[q];
     }
     __builtin_amdgcn_wave_barrier();
-    if (in_range && rank == 0) mine[d] += __popcll(same);
+    if (there && rank == 0) mine[d] += __popcll(same);
     __builtin_amdgcn_wave_barrier();
   }
 }
@@ -1217,7 +1240,10 @@ __device__ inline void best_add(Best b, int k, bool want, uint64_t key, int32_t 
     b.item[at] = item;
   }
   __syncthreads();
-  if (*b.count > kTopRoom - kThreads) least = best_cut(b, k);
+  if (*b.count > kTopRoom - kThreads) {
+    const uint64_t now = best_cut(b, k);
+    least = now > least ? now : least;
+  }
   __syncthreads();
 }
 
@@ -1244,12 +1270,13 @@ struct TopArgs {
   int32_t items, K, k, words;
   Table<T> x, w;
   const uint32_t *excluded;  // [n][words] bits (NULL: none)
-  // in pieces of the items, joined afterwards
-  int64_t per_piece;
-  int32_t pieces;
-  uint64_t *key;   // [n][pieces][k]
-  int32_t *item;
-  // or from candidates
+  const int64_t *row_ptr;    // the lists themselves
+  const int32_t *list;
+  int64_t entries;
+  // few rows: keys of the scores and the groups' largest
+  int32_t groups;
+  uint64_t *key, *most;      // [n][groups 64], [n][groups]
+  // many: candidates
   const int32_t *found, *count;  // [n][room], [n]: more than room: all items
   int32_t room;
   int32_t *out_item;
@@ -1306,40 +1333,161 @@ __device__ inline void top_out(const TopArgs<T> &a, int64_t r, Best b) {
   }
 }
 
-// The k best of a piece of the items for one row.  Bound by the reads of the items' rows.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_top_scan(TopArgs<T> a) {
-  __shared__ double x[kMaxK];
-  __shared__ uint64_t keys[kTopRoom];
-  __shared__ int32_t items[kTopRoom], count;
-  const int64_t r = blockIdx.x;
-  const int piece = blockIdx.y;
-  const Best b{keys, items, &count};
-  top_row(a, r, x, &count);
-  const int64_t j0 = piece * a.per_piece, j1 = min(j0 + a.per_piece, static_cast<int64_t>(a.items));
-  top_all(a, r, x, b, j0, j1);
-  if (a.pieces == 1) return top_out(a, r, b);
-  const int64_t to = (r * a.pieces + piece) * a.k;
-  for (int q = threadIdx.x; q < a.k; q += kThreads) {
-    a.key[to + q] = q < count ? keys[q] : 0;
-    a.item[to + q] = q < count ? items[q] : -1;
+// ---- few rows
+//
+// Scores of R rows with groups of 64 items, as keys, and each row's largest key of the group.  A row's k best lie in
+// the groups whose largest key is among the k largest of these (equal ones too), so the second kernel looks at few
+// more than k groups.  Bound by the reads of the items' rows, once for R rows, and by latency.
+constexpr int kTopGroup = 64;
+template <class T, int R>
+__global__ __launch_bounds__(kThreads) void k_top_scores(TopArgs<T> a) {
+  __shared__ double x[R][kMaxK];
+  __shared__ uint64_t most[4][R];
+  __shared__ uint64_t out[R];
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * R;
+  const int l = threadIdx.x & (kDotLanes - 1), g = threadIdx.x / kDotLanes;
+  const int64_t j0 = static_cast<int64_t>(blockIdx.x) * kTopGroup;
+  for (int q = threadIdx.x; q < R * a.K; q += kThreads) {
+    const int r = q / a.K, k = q - r * a.K;
+    if (r0 + r < a.n) x[r][k] = static_cast<double>(to_f(a.x.p[(a.row0 + r0 + r) * a.x.ld + k]));
+  }
+  for (int q = threadIdx.x; q < R * ((4 - a.K % 4) % 4); q += kThreads) x[q % R][a.K + q / R] = 0.0;  // up to a whole float4
+  if (threadIdx.x < R) out[threadIdx.x] = 0;
+  __syncthreads();
+  if (a.row_ptr) {  // the group's excluded items, a bit each
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r0 + r >= a.n) continue;
+      int64_t b, e;
+      row_range(a.row_ptr, a.entries, 0, a.row0 + r0 + r, b, e);
+      for (int64_t q = b + threadIdx.x; q < e; q += kThreads) {
+        const int64_t d = a.list[q] - j0;
+        if (d >= 0 && d < kTopGroup) atomicOr(reinterpret_cast<unsigned long long *>(&out[r]), 1ull << d);
+      }
+    }
+    __syncthreads();
+  }
+  uint64_t best[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) best[r] = 0;
+#pragma unroll 1
+  for (int q = 0; q < kTopGroup * kDotLanes / kThreads; ++q) {
+    const int d = q * (kThreads / kDotLanes) + g;
+    const int64_t j = j0 + d;
+    double s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = 0.0;
+    if (j < a.items) {
+      const T *w = a.w.p + j * a.w.ld;
+#pragma unroll(R == 8 ? 2 : 4)
+      for (int k = 4 * l; k < a.K; k += 4 * kDotLanes) {
+        const f32x4 v = load4(w, k, a.K, a.w.vec);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) s[r] = fma(x[r][k + z], static_cast<double>(v[z]), s[r]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+      for (int o = 1; o < kDotLanes; o <<= 1) s[r] += __shfl_xor(s[r], o);
+      const uint64_t key = j < a.items && !((out[r] >> d) & 1) ? max(order_key(s[r]), static_cast<uint64_t>(1)) : 0;  // 0: no item
+      best[r] = max(best[r], key);
+      if (l == 0 && j < a.items && r0 + r < a.n) a.key[(r0 + r) * a.groups * kTopGroup + j] = key;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int o = kDotLanes; o < 64; o <<= 1) best[r] = max(best[r], static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best[r]), o)));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6][r] = best[r];
+  }
+  __syncthreads();
+  if (threadIdx.x < R && r0 + threadIdx.x < a.n) {
+    const int r = threadIdx.x;
+    a.most[(r0 + r) * a.groups + blockIdx.x] = max(max(most[0][r], most[1][r]), max(most[2][r], most[3][r]));
   }
 }
 
+// The k-th largest of n keys' upper 32 bits, rounded down to their upper 22 (two histograms of 11 bits); 0 for fewer
+// than k.  value(q): the q-th.  kThreads threads
+template <class F>
+__device__ inline uint32_t kth_largest(int64_t n, int k, int32_t *hist, int32_t *sh, F value) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t prefix = 0;
+  int need = k;
+  for (int round = 0; round < 2; ++round) {
+    const int shift = round ? 10 : 21;
+    for (int b = threadIdx.x; b < 2048; b += kThreads) hist[b] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int64_t q = threadIdx.x; q < n; q += kThreads) {
+      const uint32_t u = value(q);
+      if (round == 0 || u >> 21 == prefix) atomicAdd(&hist[(u >> shift) & 2047], 1);
+    }
+    __syncthreads();
+    // digits from the largest down: thread i holds 2047 - 8i .. 2040 - 8i
+    int own = 0;
+    for (int z = 0; z < 8; ++z) own += hist[2047 - 8 * threadIdx.x - z];
+    int s = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(s, o);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) sh[wave] = s;
+    if (threadIdx.x == 0) sh[4] = -1;
+    __syncthreads();
+    int above = s - own;
+    for (int w = 0; w < wave; ++w) above += sh[w];
+    if (above < need && above + own >= need) {
+      for (int z = 0; z < 8; ++z) {
+        const int b = 2047 - 8 * threadIdx.x - z;
+        if (above + hist[b] >= need) {
+          sh[4] = b;
+          sh[5] = need - above;
+          break;
+        }
+        above += hist[b];
+      }
+    }
+    __syncthreads();
+    if (sh[4] < 0) return 0;
+    prefix = round ? prefix << 11 | sh[4] : sh[4];
+    need = sh[5];
+    __syncthreads();
+  }
+  return prefix << 10;
+}
+
+// The k best of a row from its groups' keys
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_top_join(TopArgs<T> a) {
+__global__ __launch_bounds__(kThreads) void k_top_pick(TopArgs<T> a) {
   __shared__ uint64_t keys[kTopRoom];
-  __shared__ int32_t items[kTopRoom], count;
+  __shared__ int32_t items[kTopRoom], count, groups, hist[2048], sh[6];
   const int64_t r = blockIdx.x;
-  if (threadIdx.x == 0) count = 0;
-  __syncthreads();
+  const uint64_t *most = a.most + r * a.groups;
+  if (threadIdx.x == 0) count = groups = 0;
+  const uint32_t least32 = max(kth_largest(a.groups, a.k, hist, sh, [&](int64_t q) { return static_cast<uint32_t>(most[q] >> 32); }), 1u);
   const Best b{keys, items, &count};
-  uint64_t least = 0;
-  const int64_t from = r * a.pieces * a.k, all = static_cast<int64_t>(a.pieces) * a.k;
-  for (int64_t base = 0; base < all; base += kThreads) {
-    const int64_t q = base + threadIdx.x;
-    const int32_t j = q < all ? a.item[from + q] : -1;
-    best_add(b, a.k, j >= 0, q < all ? a.key[from + q] : 0, j, least);
+  // room for the numbers of 2048 groups at a time
+  uint64_t least = static_cast<uint64_t>(least32) << 32;
+  for (int64_t g0 = 0; g0 < a.groups; g0 += 2048) {
+    const int64_t g1 = min(g0 + 2048, static_cast<int64_t>(a.groups));
+    __syncthreads();
+    if (threadIdx.x == 0) groups = 0;
+    __syncthreads();
+    for (int64_t q = g0 + threadIdx.x; q < g1; q += kThreads)
+      if (most[q] >= least) hist[atomicAdd(&groups, 1)] = static_cast<int32_t>(q);
+    __syncthreads();
+    const int n = groups;
+    for (int q = 0; q < n; q += kThreads / kTopGroup) {
+      const int at = q + threadIdx.x / kTopGroup;
+      const int64_t j = at < n ? static_cast<int64_t>(hist[at]) * kTopGroup + threadIdx.x % kTopGroup : a.items;
+      const uint64_t key = j < a.items ? a.key[r * a.groups * kTopGroup + j] : 0;
+      best_add(b, a.k, key > 0, key, static_cast<int32_t>(j), least);
+    }
   }
   best_cut(b, a.k);
   top_out(a, r, b);
@@ -1362,6 +1510,7 @@ __global__ __launch_bounds__(kThreads) void k_top_join(TopArgs<T> a) {
 constexpr int kScoreTiles = 2;   // tiles of 32 items that a step stages
 constexpr int row_room(int kc) { return kc > 25 ? 16 : 32; }  // candidates of a row that a workgroup keeps in LDS
 constexpr int kCandidates = 1024;
+constexpr double kTopAll = 1.2e9;  // scores times (numbers + 64) up to which all scores are made in 64 bits
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_top_pack(Table<T> x, Table<T> w, int64_t row0, int64_t rows, int32_t xt, _Float16 *px, _Float16 *pw,
@@ -1587,58 +1736,12 @@ __device__ inline uint32_t order_bits(float v) {
 }
 __device__ inline float bits_value(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 
-// T of each row: the k-th largest of its bounds, rounded down to the upper 22 bits (two histograms of 11 bits).  One
-// workgroup per row; bound by the reads of the bounds.
+// T of each row: the k-th largest of its bounds, rounded down.  One workgroup per row; bound by the reads of the bounds.
 __global__ __launch_bounds__(kThreads) void k_top_least(const float *most, int64_t per_row, int32_t k, float *least) {
-  __shared__ int32_t hist[2048], sh[4], digit, left;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ int32_t hist[2048], sh[6];
   const float *row = most + blockIdx.x * per_row;
-  uint32_t prefix = 0;
-  int need = k;
-  for (int round = 0; round < 2; ++round) {
-    const int shift = round ? 10 : 21;
-    for (int b = threadIdx.x; b < 2048; b += kThreads) hist[b] = 0;
-    __syncthreads();
-    for (int64_t q = threadIdx.x; q < per_row; q += kThreads) {
-      const uint32_t u = order_bits(row[q]);
-      if (round == 0 || u >> 21 == prefix) atomicAdd(&hist[(u >> shift) & 2047], 1);
-    }
-    __syncthreads();
-    // digits from the largest down: thread i holds 2047 - 8i .. 2040 - 8i
-    int own = 0;
-    for (int z = 0; z < 8; ++z) own += hist[2047 - 8 * threadIdx.x - z];
-    int s = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(s, o);
-      if (lane >= o) s += u;
-    }
-    if (lane == 63) sh[wave] = s;
-    if (threadIdx.x == 0) digit = -1;
-    __syncthreads();
-    int above = s - own;
-    for (int w = 0; w < wave; ++w) above += sh[w];
-    if (above < need && above + own >= need) {
-      for (int z = 0; z < 8; ++z) {
-        const int b = 2047 - 8 * threadIdx.x - z;
-        if (above + hist[b] >= need) {
-          digit = b;
-          left = need - above;
-          break;
-        }
-        above += hist[b];
-      }
-    }
-    __syncthreads();
-    if (digit < 0) {  // fewer than k bounds
-      if (threadIdx.x == 0) least[blockIdx.x] = -__builtin_inff();
-      return;
-    }
-    prefix = round ? prefix << 11 | digit : digit;
-    need = left;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) least[blockIdx.x] = bits_value(prefix << 10);
+  const uint32_t u = kth_largest(per_row, k, hist, sh, [&](int64_t q) { return order_bits(row[q]); });
+  if (threadIdx.x == 0) least[blockIdx.x] = u ? bits_value(u) : -__builtin_inff();
 }
 
 // The candidates of a row (or all items) in order
@@ -1685,7 +1788,7 @@ __global__ __launch_bounds__(kThreads) void k_exclude(const int64_t *row_ptr, co
 struct ps_soft {
   int64_t items = 0;
   int32_t K = 0, type = 0;
-  int32_t splits = 0;
+  int32_t splits = 0, search = -1;
   int device = -1;
   bool opened = false;
   hipStream_t stream = nullptr;  // NULL: HIP's null stream
@@ -1799,6 +1902,12 @@ struct Arena {
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 unsigned blocks_for(int64_t n, int64_t per, int64_t most) {
   return static_cast<unsigned>(std::max<int64_t>(1, std::min(up(n, per), most)));
+}
+
+int32_t row_lanes(int32_t K) {  // lanes of 4 numbers for a row, a power of two
+  int32_t n = 1;
+  while (4 * n < K) n *= 2;
+  return n;
 }
 
 template <class T>
@@ -1980,7 +2089,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       hipLaunchKernelGGL(k_fill_keys, dim3(blocks_for(t.entries, kThreads * 4, 4096)), dim3(kThreads), 0, s, t.key, t.entries, t.dead);
     const unsigned row_blocks = blocks_for(t.n, 4, kRowParts);
     hipLaunchKernelGGL((k_targets<Distill>), dim3(row_blocks), dim3(kThreads), 0, s, t);
-    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kThreads), 0, s, x, w, h->K, at_f(p.part));
+    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kScanThreads), 0, s, x, w, h->K, row_lanes(h->K), at_f(p.part));
     const PackSide sx{px, p.x_stride, static_cast<int32_t>(p.xt), dw}, sw{pw, p.w_stride, static_cast<int32_t>(p.wt), dx};
     hipLaunchKernelGGL((k_pack<T, NP>), dim3(static_cast<unsigned>(p.xt + p.wt)), dim3(kThreads),
                        static_cast<unsigned>(kTile * (std::min(p.kd, kPackBlocks) * 32 + 1) * 4), s, x, w, sx, sw, h->K, p.k16, p.kd, at_f(p.part),
@@ -2083,18 +2192,21 @@ int32_t score_chunks(int32_t K) {
 struct TopPlan {
   bool filter;
   int64_t rows;  // rows of one launch: what they need stays near a gigabyte
-  int64_t per;
-  int32_t pieces, words, kc;
+  int32_t words, kc, groups;
   int64_t xt, wt, steps, per_split;
   int32_t splits;
-  int64_t bits, key, item, part, px, pw, most, least, found, count, bytes;
+  int64_t bits, key, maxima, part, px, pw, most, least, found, count, bytes;
 };
 
 TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
   TopPlan p{};
   const int64_t all = std::max<int64_t>(n, 1);
   p.words = static_cast<int32_t>(up(h->items, 32));
-  p.filter = all > 32 && h->items > 2048 && h->items < 1 << 30;
+  // All scores in 64 bits, or candidates first: 64 bits take about 60 ps a score of 64 numbers and its key, the search
+  // 60 us at least
+  p.filter = static_cast<double>(all) * static_cast<double>(h->items) * (h->K + 64) > kTopAll && h->items > 2048;
+  if (h->search >= 0) p.filter = h->search == 1;
+  p.filter = p.filter && h->items < 1 << 30;  // counts of candidates
   Arena a;
   if (p.filter) {
     p.kc = score_chunks(h->K);
@@ -2113,17 +2225,14 @@ TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
     p.least = a.take(p.rows * 4);
     p.found = a.take(p.rows * kCandidates * 4);
     p.count = a.take(p.rows * 4);
+    p.bits = a.take(exclude ? p.rows * p.words * 4 : 0);
   } else {
-    p.pieces = static_cast<int32_t>(std::max<int64_t>(1, std::min({up(512, all), up(h->items, kThreads), static_cast<int64_t>(256)})));
-    if (h->splits > 0) p.pieces = static_cast<int32_t>(std::min<int64_t>(h->splits, h->items));
-    p.per = up(h->items, p.pieces);
-    p.pieces = static_cast<int32_t>(up(h->items, p.per));
-    const int64_t per_row = (exclude ? p.words * 4LL : 0) + static_cast<int64_t>(p.pieces) * k * 12;
-    p.rows = std::min(all, std::max<int64_t>(1, (1LL << 30) / per_row));
-    p.key = a.take(p.rows * p.pieces * k * 8);
-    p.item = a.take(p.rows * p.pieces * k * 4);
+    p.groups = static_cast<int32_t>(up(h->items, kTopGroup));
+    p.rows = std::min(all, std::max<int64_t>(1, (1LL << 30) / (p.groups * (kTopGroup + 1) * 8LL)));
+    p.rows = std::min<int64_t>(p.rows, 32768);  // rows are the launch's second dimension
+    p.key = a.take(p.rows * p.groups * kTopGroup * 8);
+    p.maxima = a.take(p.rows * p.groups * 8);
   }
-  p.bits = a.take(exclude ? p.rows * p.words * 4 : 0);
   p.bytes = a.at;
   return p;
 }
@@ -2164,10 +2273,12 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
   a.w = Table<T>{W, ldw, h->items, aligned4(W, ldw), nullptr};
   uint32_t *bits = reinterpret_cast<uint32_t *>(base + p.bits);
   a.excluded = row_ptr ? bits : nullptr;
-  a.per_piece = p.per;
-  a.pieces = p.pieces;
+  a.row_ptr = row_ptr;
+  a.list = item;
+  a.entries = entries;
+  a.groups = p.groups;
   a.key = reinterpret_cast<uint64_t *>(base + p.key);
-  a.item = reinterpret_cast<int32_t *>(base + p.item);
+  a.most = reinterpret_cast<uint64_t *>(base + p.maxima);
   a.found = reinterpret_cast<int32_t *>(base + p.found);
   a.count = reinterpret_cast<int32_t *>(base + p.count);
   a.room = kCandidates;
@@ -2176,19 +2287,22 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
   a.ldo = ldo;
   float *part = reinterpret_cast<float *>(base + p.part);
   if (p.filter && h->type != PS_SOFT_F16)
-    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kThreads), 0, s, a.x, a.w, h->K, part);
+    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kScanThreads), 0, s, a.x, a.w, h->K, row_lanes(h->K), part);
   for (a.row0 = 0; a.row0 < n; a.row0 += p.rows) {
     a.n = std::min(p.rows, n - a.row0);
     const unsigned rows = static_cast<unsigned>(a.n);
+    if (!p.filter) {
+      const unsigned groups = static_cast<unsigned>(p.groups);
+      if (a.n >= 8) hipLaunchKernelGGL((k_top_scores<T, 8>), dim3(groups, (rows + 7) / 8), dim3(kThreads), 0, s, a);
+      else if (a.n >= 3) hipLaunchKernelGGL((k_top_scores<T, 4>), dim3(groups, (rows + 3) / 4), dim3(kThreads), 0, s, a);
+      else hipLaunchKernelGGL((k_top_scores<T, 1>), dim3(groups, rows), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL((k_top_pick<T>), dim3(rows), dim3(kThreads), 0, s, a);
+      continue;
+    }
     if (row_ptr) {
       hipLaunchKernelGGL(k_clear, dim3(blocks_for(a.n * p.words, kThreads * 4, 8192)), dim3(kThreads), 0, s, bits, a.n * p.words);
       hipLaunchKernelGGL(k_exclude, dim3(static_cast<unsigned>(up(a.n, 4))), dim3(kThreads), 0, s, row_ptr, item, entries, a.row0,
                          a.n, a.items, p.words, bits);
-    }
-    if (!p.filter) {
-      hipLaunchKernelGGL((k_top_scan<T>), dim3(rows, static_cast<unsigned>(p.pieces)), dim3(kThreads), 0, s, a);
-      if (p.pieces > 1) hipLaunchKernelGGL((k_top_join<T>), dim3(rows), dim3(kThreads), 0, s, a);
-      continue;
     }
     ScoreArgs q{};
     _Float16 *px = reinterpret_cast<_Float16 *>(base + p.px), *pw = reinterpret_cast<_Float16 *>(base + p.pw);
@@ -2288,6 +2402,10 @@ int ps_soft_set_option(ps_soft_t *h, int32_t key, int64_t value) {
     case PS_SOFT_OPT_SPLITS:
       if (value < 0 || value > 1024) return fail(h, PS_SOFT_EINVAL, "pieces must be in [0, 1024]");
       h->splits = static_cast<int32_t>(value);
+      return PS_SOFT_OK;
+    case PS_SOFT_OPT_SEARCH:
+      if (value < -1 || value > 1) return fail(h, PS_SOFT_EINVAL, "the search's form must be in [-1, 1]");
+      h->search = static_cast<int32_t>(value);
       return PS_SOFT_OK;
     default:
       return fail(h, PS_SOFT_EINVAL, "unknown option key %d", key);

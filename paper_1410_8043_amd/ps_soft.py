@@ -19,7 +19,7 @@ from paper_1410_8043_amd import ps_mf as _mf
 LIB_PATH = _mf.LIB_PATH
 OK, EINVAL, ENOMEM, EDEVICE, ESTATE = 0, -1, -2, -3, -4
 F32, BF16, F16 = 0, 1, 2
-OPT_DEVICE, OPT_SPLITS = 1, 2
+OPT_DEVICE, OPT_SPLITS, OPT_SEARCH = 1, 2, 3
 TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 MAX_TOP = 256
 
@@ -79,10 +79,11 @@ class PsSoft:
     """A handle for tables of ``items`` rows of K numbers: its calls share a workspace that grows to the
     largest call (``reserve`` grows it ahead, as a call that will be captured into a graph needs).
 
-    ``splits`` forces the number of pieces that the reduced axis is cut into (0: by the sizes).
+    ``splits`` forces the number of pieces that the reduced axis is cut into (0: by the sizes), ``search`` the form of
+    ``top`` (0: all scores in 64 bits, 1: candidates first, None: by the sizes; same results).
     """
 
-    def __init__(self, items, K, dtype=torch.float32, *, device=None, splits=0):
+    def __init__(self, items, K, dtype=torch.float32, *, device=None, splits=0, search=None):
         if dtype not in TYPES:
             raise ValueError(f"dtype must be one of {', '.join(map(str, TYPES))}, not {dtype}")
         self.items, self.K, self.dtype = int(items), int(K), dtype
@@ -92,6 +93,8 @@ class PsSoft:
         try:
             if splits:
                 _check(self.h, "ps_soft_set_option", _lib.ps_soft_set_option(self.h, OPT_SPLITS, int(splits)))
+            if search is not None:
+                _check(self.h, "ps_soft_set_option", _lib.ps_soft_set_option(self.h, OPT_SEARCH, int(search)))
             if device is not None:
                 self._open(torch.device("cuda", device) if isinstance(device, int) else torch.device(device))
         except Exception:

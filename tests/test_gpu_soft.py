@@ -221,13 +221,13 @@ def test_distill(soft, n, M, K, k, tau, full, splits, dtype):
 @pytest.mark.parametrize("n,M,K,k,mean,splits", [(1, 1, 1, 1, 0, 0), (1, 50, 8, 60, 5, 0), (3, 300, 17, 256, 0, 0), (33, 700, 64, 10, 40, 3),
                                                  (200, 1111, 100, 64, 0, 0), (7, 20_000, 128, 100, 300, 0), (20, 900, 512, 5, 9, 0),
                                                  (600, 5000, 32, 20, 30, 0), (1, 100_000, 48, 256, 50, 0)])
-def test_top(soft, n, M, K, k, mean, splits, dtype):
+def test_top(soft, n, M, K, k, mean, splits, dtype, search=None):
     g = gen(5, n, M, K)
     X, W = tables(n, M, K, dtype, g)
     ptr, item = lists(n, M, mean, g) if mean else (None, None)
     want, score = soft_ref.top(X, W, k, ptr, item)
     say(f"top n={n} M={M} K={K} k={k} {dtype}")
-    with soft.PsSoft(M, K, dtype, splits=splits) as h:
+    with soft.PsSoft(M, K, dtype, splits=splits, search=search) as h:
         got = h.top(X, W, k, row_ptr=ptr, item=item)
     assert np.array_equal(got[0].cpu().numpy(), want)
     # the 64-bit sum in another order, rounded to fp32: at most a step of fp32 apart
@@ -243,8 +243,41 @@ def test_top(soft, n, M, K, k, mean, splits, dtype):
                                                  (64, 2300, 256, 7, 0, 0), (34, 2400, 300, 40, 9, 0), (90, 2222, 512, 12, 0, 0),
                                                  (1000, 20_011, 40, 50, 100, 0)])
 def test_top_of_many_rows(soft, n, M, K, k, mean, splits, dtype):
-    # enough rows and items for the search by candidates
-    test_top(soft, n, M, K, k, mean, splits, dtype)
+    # both searches
+    test_top(soft, n, M, K, k, mean, splits, dtype, 0)
+    test_top(soft, n, M, K, k, mean, splits, dtype, 1)
+
+
+@pytest.mark.parametrize("n,M,K,k", [(1, 1, 1, 1), (3, 40, 7, 50), (70, 500, 33, 256), (9, 2000, 64, 100)])
+def test_top_by_candidates_of_few_items(soft, n, M, K, k):
+    # no threshold, more candidates than room: forms that the sizes would not choose
+    test_top(soft, n, M, K, k, 5 if M > 20 else 0, 0, F32, 1)
+
+
+def test_top_forms_agree(soft):
+    # the largest case that both take in a moment, bit for bit
+    g = gen(22)
+    for n, M, K, k, dtype in ((3000, 17_770, 128, 64, F32), (700, 30_011, 100, 200, F16), (4100, 5000, 64, 10, BF16)):
+        X, W = tables(n, M, K, dtype, g)
+        ptr, item = lists(n, M, 50, g)
+        say(f"top forms n={n} M={M} K={K} k={k} {dtype}")
+        with soft.PsSoft(M, K, dtype, search=0) as a, soft.PsSoft(M, K, dtype, search=1) as b, soft.PsSoft(M, K, dtype) as c:
+            x, y, z = (h.top(X, W, k, row_ptr=ptr, item=item) for h in (a, b, c))
+        assert same(x, y) and same(x, z)
+
+
+def test_equal_calls_give_equal_bits(soft):
+    # several tiles and pieces, enough workgroups that their order differs from call to call
+    g = gen(23)
+    for n, M, K, dtype in ((4096, 9000, 128, F32), (1500, 20_000, 256, BF16), (5000, 3000, 512, F32), (700, 4000, 40, F16)):
+        X, W = tables(n, M, K, dtype, g)
+        ptr, item = lists(n, M, 30, g)
+        for splits in (0, 16, 5):
+            say(f"equal bits n={n} M={M} K={K} {dtype} splits={splits}")
+            with soft.PsSoft(M, K, dtype, splits=splits) as h:
+                first = h.xent(X, W, item, row_ptr=ptr)
+                for _ in range(8):
+                    assert same(h.xent(X, W, item, row_ptr=ptr), first)
 
 
 def test_top_of_uneven_tables(soft):
@@ -268,8 +301,9 @@ def test_top_of_uneven_tables(soft):
             w[777, 5] = float(name)
         want, score = soft_ref.top(X, w, k, ptr, item)
         say(f"top uneven {name}")
-        with soft.PsSoft(M, K) as h:
+        with soft.PsSoft(M, K, search=0) as h, soft.PsSoft(M, K, search=1) as h1:
             best, val = h.top(X, w, k, row_ptr=ptr.cuda(), item=item)
+            assert same((best, val), h1.top(X, w, k, row_ptr=ptr.cuda(), item=item))
         got = best.cpu().numpy()
         if name == "finite":
             # equal up to the order of scores whose 64-bit sums differ in their last bits
@@ -290,7 +324,8 @@ def test_top_of_uneven_tables(soft):
                     assert 777 not in got[i]
 
 
-def test_top_ties_masks_and_nan(soft):
+@pytest.mark.parametrize("search", [0, 1])
+def test_top_ties_masks_and_nan(soft, search):
     # whole numbers: many equal scores, exact in any order; the lowest items win
     g = gen(6)
     n, M, K, k = 50, 4000, 8, 100
@@ -303,7 +338,7 @@ def test_top_ties_masks_and_nan(soft):
     item = torch.cat((torch.arange(M), torch.arange(3, M))).int().cuda()
     want, score = soft_ref.top(X, W, k, ptr, item)
     say("top ties")
-    with soft.PsSoft(M, K) as h:
+    with soft.PsSoft(M, K, search=search) as h:
         best, val = h.top(X, W, k, row_ptr=ptr.cuda(), item=item)
         W2 = W.clone()
         W2[1234, 3] = float("nan")

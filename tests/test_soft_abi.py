@@ -23,7 +23,8 @@ def test_header_and_binding_name_the_same_functions():
     for name in names:
         assert getattr(ps_soft._lib, name)
     for py, c in (("EINVAL", "EINVAL"), ("ENOMEM", "ENOMEM"), ("EDEVICE", "EDEVICE"), ("ESTATE", "ESTATE"), ("F32", "F32"),
-                  ("BF16", "BF16"), ("F16", "F16"), ("OPT_DEVICE", "OPT_DEVICE"), ("OPT_SPLITS", "OPT_SPLITS")):
+                  ("BF16", "BF16"), ("F16", "F16"), ("OPT_DEVICE", "OPT_DEVICE"), ("OPT_SPLITS", "OPT_SPLITS"),
+                  ("OPT_SEARCH", "OPT_SEARCH")):
         m = re.search(r"#define PS_SOFT_%s \(?(-?\d+)\)?" % c, text)
         assert m and int(m.group(1)) == getattr(ps_soft, py)
 
@@ -56,7 +57,7 @@ def handle():
 
 
 @pytest.mark.parametrize("key,value", [(0, 0), (99, 0), (ps_soft.OPT_DEVICE, -2), (ps_soft.OPT_DEVICE, 4096), (ps_soft.OPT_SPLITS, -1),
-                                       (ps_soft.OPT_SPLITS, 1025)])
+                                       (ps_soft.OPT_SPLITS, 1025), (ps_soft.OPT_SEARCH, -2), (ps_soft.OPT_SEARCH, 2)])
 def test_options_refused(handle, key, value):
     assert ps_soft._lib.ps_soft_set_option(handle, key, value) == ps_soft.EINVAL
     assert ps_soft._lib.ps_soft_last_error(handle)
