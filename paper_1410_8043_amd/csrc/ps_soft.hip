@@ -1250,6 +1250,56 @@ __device__ inline void best_add(Best b, int k, bool want, uint64_t key, int32_t 
 // A score in 64 bits: products of the tables' numbers are exact, and the sum has one order everywhere: 8 lanes of 4
 // numbers each take every eighth 4, then the lanes are added in pairs.
 constexpr int kDotLanes = 8;
+template <int Move>
+__device__ inline double moved(double v) {  // of another lane of the 8: 0xb1 of the pair, 0x4e of the other pair, 0x141 of the other four
+  const unsigned long long u = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), Move, 0xf, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), Move, 0xf, 0xf, false);
+  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo)));
+}
+__device__ inline double sum8(double s) {
+  s += moved<0xb1>(s);
+  s += moved<0x4e>(s);
+  return s + moved<0x141>(s);
+}
+// Of lane l ^ 4: two moves, each for half of the lanes
+__device__ inline int far4(int v) {
+  const int up = __builtin_amdgcn_update_dpp(0, v, 0x104, 0xf, 0x5, false);  // lanes 0..3 and 8..11 of 16 take l + 4
+  return __builtin_amdgcn_update_dpp(up, v, 0x114, 0xf, 0xa, false);         // the others l - 4
+}
+__device__ inline double far4(double v) {
+  const unsigned long long u = __double_as_longlong(v);
+  const uint32_t lo = static_cast<uint32_t>(far4(static_cast<int>(u))), hi = static_cast<uint32_t>(far4(static_cast<int>(u >> 32)));
+  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
+}
+// The sums of R numbers over 8 lanes, sum8's order: lane l gets number spread_of<R>(l), 8 / R lanes each.  Each step halves
+// what a lane holds, so 8 numbers take 7 additions instead of 24
+template <int R>
+__device__ inline int spread_of(int l) {
+  return R == 8 ? (l & 1) << 2 | (l & 2) | l >> 2 : R == 4 ? (l & 1) << 1 | (l >> 1 & 1) : 0;
+}
+template <int R>
+__device__ inline double spread8(double (&s)[R], int l) {
+  static_assert(R == 1 || R == 4 || R == 8, "1, 4 or 8 numbers");
+  if constexpr (R == 1) {
+    return sum8(s[0]);
+  } else {
+    double a[R / 2], b[R / 4];
+    const bool odd = l & 1, second = l & 2, far = l & 4;
+#pragma unroll
+    for (int i = 0; i < R / 2; ++i) {
+      const double keep = odd ? s[R / 2 + i] : s[i], give = odd ? s[i] : s[R / 2 + i];
+      a[i] = keep + moved<0xb1>(give);
+    }
+#pragma unroll
+    for (int i = 0; i < R / 4; ++i) {
+      const double keep = second ? a[R / 4 + i] : a[i], give = second ? a[i] : a[R / 4 + i];
+      b[i] = keep + moved<0x4e>(give);
+    }
+    if constexpr (R == 4) return b[0] + far4(b[0]);
+    else return (far ? b[1] : b[0]) + far4(far ? b[0] : b[1]);
+  }
+}
 template <class T>
 __device__ inline double dot64(const double *x, const T *w, int l, int K, bool vec) {
   double s = 0.0;
@@ -1259,9 +1309,7 @@ __device__ inline double dot64(const double *x, const T *w, int l, int K, bool v
 #pragma unroll
     for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);
   }
-#pragma unroll
-  for (int o = 1; o < kDotLanes; o <<= 1) s += __shfl_xor(s, o);
-  return s;
+  return sum8(s);
 }
 
 template <class T>
@@ -1337,76 +1385,74 @@ __device__ inline void top_out(const TopArgs<T> &a, int64_t r, Best b) {
 //
 // Scores of R rows with groups of 64 items, as keys, and each row's largest key of the group.  A row's k best lie in
 // the groups whose largest key is among the k largest of these (equal ones too), so the second kernel looks at few
-// more than k groups.  Bound by the reads of the items' rows, once for R rows, and by latency.
-constexpr int kTopGroup = 64;
+// more than k groups.  A workgroup takes `per` groups, so that many rows load their numbers and lists less often.
+// Bound by the reads of the items' rows, once for R rows, and by latency.
+constexpr int kTopGroup = 64, kTopGroups = 8;  // items of a group; most groups of a workgroup
 template <class T, int R>
-__global__ __launch_bounds__(kThreads) void k_top_scores(TopArgs<T> a) {
+__global__ __launch_bounds__(kThreads) void k_top_scores(TopArgs<T> a, int per) {
   __shared__ double x[R][kMaxK];
-  __shared__ uint64_t most[4][R];
-  __shared__ uint64_t out[R];
+  __shared__ uint64_t most[2][4][R];
+  __shared__ uint64_t out[R][kTopGroups];
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * R;
   const int l = threadIdx.x & (kDotLanes - 1), g = threadIdx.x / kDotLanes;
-  const int64_t j0 = static_cast<int64_t>(blockIdx.x) * kTopGroup;
+  const int g0 = blockIdx.x * per, g1 = min(g0 + per, a.groups);
   for (int q = threadIdx.x; q < R * a.K; q += kThreads) {
     const int r = q / a.K, k = q - r * a.K;
     if (r0 + r < a.n) x[r][k] = static_cast<double>(to_f(a.x.p[(a.row0 + r0 + r) * a.x.ld + k]));
   }
   for (int q = threadIdx.x; q < R * ((4 - a.K % 4) % 4); q += kThreads) x[q % R][a.K + q / R] = 0.0;  // up to a whole float4
-  if (threadIdx.x < R) out[threadIdx.x] = 0;
+  if (threadIdx.x < R * kTopGroups) out[threadIdx.x / kTopGroups][threadIdx.x % kTopGroups] = 0;
   __syncthreads();
-  if (a.row_ptr) {  // the group's excluded items, a bit each
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
+  if (a.row_ptr) {  // the groups' excluded items, a bit each
+    constexpr int W = R < 4 ? R : 4, L = kThreads / W;  // rows at a time, threads each
+    for (int r = threadIdx.x / L; r < R; r += W) {
       if (r0 + r >= a.n) continue;
       int64_t b, e;
       row_range(a.row_ptr, a.entries, 0, a.row0 + r0 + r, b, e);
-      for (int64_t q = b + threadIdx.x; q < e; q += kThreads) {
-        const int64_t d = a.list[q] - j0;
-        if (d >= 0 && d < kTopGroup) atomicOr(reinterpret_cast<unsigned long long *>(&out[r]), 1ull << d);
+#pragma unroll 4
+      for (int64_t q = b + threadIdx.x % L; q < e; q += L) {
+        const int64_t d = a.list[q] - static_cast<int64_t>(g0) * kTopGroup;
+        if (d >= 0 && d < per * kTopGroup) atomicOr(reinterpret_cast<unsigned long long *>(&out[r][d / kTopGroup]), 1ull << (d % kTopGroup));
       }
     }
     __syncthreads();
   }
-  uint64_t best[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) best[r] = 0;
+  const int row = spread_of<R>(l);  // whose scores this lane ends up with
+  for (int at = g0; at < g1; ++at) {
+    const int64_t j0 = static_cast<int64_t>(at) * kTopGroup;
+    uint64_t best = 0;
 #pragma unroll 1
-  for (int q = 0; q < kTopGroup * kDotLanes / kThreads; ++q) {
-    const int d = q * (kThreads / kDotLanes) + g;
-    const int64_t j = j0 + d;
-    double s[R];
+    for (int q = 0; q < kTopGroup * kDotLanes / kThreads; ++q) {
+      const int d = q * (kThreads / kDotLanes) + g;
+      const int64_t j = j0 + d;
+      double s[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = 0.0;
-    if (j < a.items) {
-      const T *w = a.w.p + j * a.w.ld;
+      for (int r = 0; r < R; ++r) s[r] = 0.0;
+      if (j < a.items) {
+        const T *w = a.w.p + j * a.w.ld;
 #pragma unroll(R == 8 ? 2 : 4)
-      for (int k = 4 * l; k < a.K; k += 4 * kDotLanes) {
-        const f32x4 v = load4(w, k, a.K, a.w.vec);
+        for (int k = 4 * l; k < a.K; k += 4 * kDotLanes) {
+          const f32x4 v = load4(w, k, a.K, a.w.vec);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+          for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int z = 0; z < 4; ++z) s[r] = fma(x[r][k + z], static_cast<double>(v[z]), s[r]);
+            for (int z = 0; z < 4; ++z) s[r] = fma(x[r][k + z], static_cast<double>(v[z]), s[r]);
+        }
       }
+      const double sum = spread8<R>(s, l);
+      const uint64_t key = j < a.items && !((out[row][at - g0] >> d) & 1) ? max(order_key(sum), static_cast<uint64_t>(1)) : 0;  // 0: no item
+      best = max(best, key);
+      if (l < (R == 8 ? 8 : R) && j < a.items && r0 + row < a.n) a.key[(r0 + row) * a.groups * kTopGroup + j] = key;
     }
+    uint64_t(*const m)[R] = most[at & 1];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-      for (int o = 1; o < kDotLanes; o <<= 1) s[r] += __shfl_xor(s[r], o);
-      const uint64_t key = j < a.items && !((out[r] >> d) & 1) ? max(order_key(s[r]), static_cast<uint64_t>(1)) : 0;  // 0: no item
-      best[r] = max(best[r], key);
-      if (l == 0 && j < a.items && r0 + r < a.n) a.key[(r0 + r) * a.groups * kTopGroup + j] = key;
+    for (int o = kDotLanes; o < 64; o <<= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), o)));
+    if ((threadIdx.x & 63) < R) m[threadIdx.x >> 6][row] = best;
+    __syncthreads();
+    if (threadIdx.x < R && r0 + threadIdx.x < a.n) {
+      const int r = threadIdx.x;
+      a.most[(r0 + r) * a.groups + at] = max(max(m[0][r], m[1][r]), max(m[2][r], m[3][r]));
     }
-  }
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-#pragma unroll
-    for (int o = kDotLanes; o < 64; o <<= 1) best[r] = max(best[r], static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best[r]), o)));
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6][r] = best[r];
-  }
-  __syncthreads();
-  if (threadIdx.x < R && r0 + threadIdx.x < a.n) {
-    const int r = threadIdx.x;
-    a.most[(r0 + r) * a.groups + blockIdx.x] = max(max(most[0][r], most[1][r]), max(most[2][r], most[3][r]));
   }
 }
 
@@ -1510,7 +1556,6 @@ __global__ __launch_bounds__(kThreads) void k_top_pick(TopArgs<T> a) {
 constexpr int kScoreTiles = 2;   // tiles of 32 items that a step stages
 constexpr int row_room(int kc) { return kc > 25 ? 16 : 32; }  // candidates of a row that a workgroup keeps in LDS
 constexpr int kCandidates = 1024;
-constexpr double kTopAll = 1.2e9;  // scores times (numbers + 64) up to which all scores are made in 64 bits
 
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_top_pack(Table<T> x, Table<T> w, int64_t row0, int64_t rows, int32_t xt, _Float16 *px, _Float16 *pw,
@@ -2198,13 +2243,20 @@ struct TopPlan {
   int64_t bits, key, maxima, part, px, pw, most, least, found, count, bytes;
 };
 
+// The form estimated faster, in us.  Measured (all scores / candidates): 64 rows x 17,770 items K = 64 30 / 77, 256 rows
+// 66 / 79, 1024 rows 180 / 89; 256 rows x 100,000 items K = 16 160 / 75; 8 rows x 100,000 K = 256 43 / 135
+bool top_by_candidates(int64_t n, int64_t items, int32_t K) {
+  const double scores = static_cast<double>(n) * static_cast<double>(items);
+  const double all = 17.0 + scores * (5.0 + 0.065 * K) * 1e-6;
+  const double candidates = 60.0 + 0.2 * K + 0.01 * n + items * 1e-6 * K + scores * 0.006e-6 * K;
+  return all > candidates;
+}
+
 TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
   TopPlan p{};
   const int64_t all = std::max<int64_t>(n, 1);
   p.words = static_cast<int32_t>(up(h->items, 32));
-  // All scores in 64 bits, or candidates first: 64 bits take about 60 ps a score of 64 numbers and its key, the search
-  // 60 us at least
-  p.filter = static_cast<double>(all) * static_cast<double>(h->items) * (h->K + 64) > kTopAll && h->items > 2048;
+  p.filter = top_by_candidates(all, h->items, h->K);
   if (h->search >= 0) p.filter = h->search == 1;
   p.filter = p.filter && h->items < 1 << 30;  // counts of candidates
   Arena a;
@@ -2292,10 +2344,12 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
     a.n = std::min(p.rows, n - a.row0);
     const unsigned rows = static_cast<unsigned>(a.n);
     if (!p.filter) {
-      const unsigned groups = static_cast<unsigned>(p.groups);
-      if (a.n >= 8) hipLaunchKernelGGL((k_top_scores<T, 8>), dim3(groups, (rows + 7) / 8), dim3(kThreads), 0, s, a);
-      else if (a.n >= 3) hipLaunchKernelGGL((k_top_scores<T, 4>), dim3(groups, (rows + 3) / 4), dim3(kThreads), 0, s, a);
-      else hipLaunchKernelGGL((k_top_scores<T, 1>), dim3(groups, rows), dim3(kThreads), 0, s, a);
+      const int64_t at_once = a.n >= 8 ? 8 : a.n >= 3 ? 4 : 1, blocks = up(a.n, at_once);
+      const int32_t per = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(kTopGroups, p.groups * blocks / 768)));
+      const dim3 grid(static_cast<unsigned>(up(p.groups, per)), static_cast<unsigned>(blocks));
+      if (at_once == 8) hipLaunchKernelGGL((k_top_scores<T, 8>), grid, dim3(kThreads), 0, s, a, per);
+      else if (at_once == 4) hipLaunchKernelGGL((k_top_scores<T, 4>), grid, dim3(kThreads), 0, s, a, per);
+      else hipLaunchKernelGGL((k_top_scores<T, 1>), grid, dim3(kThreads), 0, s, a, per);
       hipLaunchKernelGGL((k_top_pick<T>), dim3(rows), dim3(kThreads), 0, s, a);
       continue;
     }
