@@ -892,24 +892,28 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     row_range(a.t.row_ptr, a.t.entries, a.t.k, i, b, e);
     const int64_t src = a.t.score ? i * a.t.ldt - b : 0;
     const float z = a.t.score ? a.t.logz[i] : 0.f;
-    for (int64_t q = b + grp; q < e; q += NG * RF) {
-      int32_t key[RF];
-      float c[RF];
-      f32x4 w[RF][V];
+    int32_t key[RF], coming[RF];
+    float c[RF], soon[RF];
+    auto read_list = [&](int64_t q) {  // a round ahead: its items' rows wait for it
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
         const int64_t at = q + f * NG;
-        key[f] = at < e ? a.t.item[at + src] : -1;
-        if (key[f] >= a.t.items) key[f] = -1;
-        c[f] = 0.f;
-        if (key[f] >= 0) c[f] = a.t.score ? a.t.score[at + src] : a.t.value ? a.t.value[at] : 1.f;
+        coming[f] = at < e ? a.t.item[at + src] : -1;
+        soon[f] = at < e ? a.t.score ? a.t.score[at + src] : a.t.value ? a.t.value[at] : 1.f : 0.f;
       }
+    };
+    read_list(b + grp);
+    for (int64_t q = b + grp; q < e; q += NG * RF) {
+      f32x4 w[RF][V];
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
+        key[f] = coming[f] < a.t.items ? coming[f] : -1;
+        c[f] = key[f] >= 0 ? soon[f] : 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) w[f][v] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (key[f] >= 0) load_row<T, G, V>(w[f], a.w.p + key[f] * a.w.ld, g, a.K, a.w.vec);
       }
+      read_list(q + NG * RF);
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
         if (a.t.score) {
@@ -1070,11 +1074,21 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out,
   // where each digit starts: the digits before it, four per thread
   const int b0 = 4 * threadIdx.x;
   int32_t v[4], at[4], s = 0;
+  if (blocks == 1) {  // one workgroup's counts are the totals
+    __syncthreads();
 #pragma unroll
-  for (int z = 0; z < 4; ++z) {
-    v[z] = b0 + z < bins ? total[b0 + z] : 0;
-    at[z] = b0 + z < bins ? hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x] : 0;
-    s += v[z];
+    for (int z = 0; z < 4; ++z) {
+      v[z] = b0 + z < bins ? cnt[0][b0 + z] + cnt[1][b0 + z] + cnt[2][b0 + z] + cnt[3][b0 + z] : 0;
+      at[z] = 0;
+      s += v[z];
+    }
+  } else {
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      v[z] = b0 + z < bins ? total[b0 + z] : 0;
+      at[z] = b0 + z < bins ? hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x] : 0;
+      s += v[z];
+    }
   }
   const int32_t own = s;
 #pragma unroll
@@ -1672,24 +1686,40 @@ __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
   if constexpr (Find) {
     have[threadIdx.x] = 0;
   }
-  if (s0 < s1) fetch(s0, 0);
+  // the rows' excluded bits of a step's tiles, read a step ahead
+  uint32_t bits[2][kScoreTiles], coming[2][kScoreTiles];
+  auto read_bits = [&](uint32_t (&to)[2][kScoreTiles], int64_t step) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int z = 0; z < kScoreTiles; ++z) {
+        const int64_t t = step * kScoreTiles + z;
+        to[u][z] = a.excluded && row[u] >= 0 && t < a.words ? a.excluded[row[u] * a.words + t] : 0u;
+      }
+  };
+  if (s0 < s1) {
+    fetch(s0, 0);
+    read_bits(coming, s0);
+  }
   for (int64_t st = s0; st < s1; ++st) {
     const int at = static_cast<int>(st - s0) & 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (st + 1 < s1) fetch(st + 1, at ^ 1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int z = 0; z < kScoreTiles; ++z) bits[u][z] = coming[u][z];
+    if (st + 1 < s1) {
+      fetch(st + 1, at ^ 1);
+      read_bits(coming, st + 1);
+    }
     float most[2][kScoreTiles];
 #pragma unroll
     for (int z = 0; z < kScoreTiles; ++z) {
       const int64_t t = st * kScoreTiles + z;
       most[0][z] = most[1][z] = -__builtin_inff();
       if (t >= a.tiles) continue;
-      uint32_t out[2] = {0u, 0u};
-      if (a.excluded) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if (row[u] >= 0) out[u] = a.excluded[row[u] * a.words + t] >> (4 * half);
-      }
+      const uint32_t out[2] = {bits[0][z] >> (4 * half), bits[1][z] >> (4 * half)};
       f32x16 s[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -1982,11 +2012,13 @@ int32_t padded_chunks(int32_t K) {
 
 // Pieces of the reduced axis, each its own workgroups: enough of them for 256 CUs three times over, and a multiple
 // of 8 where the axis is long: workgroup b runs on XCD b mod 8 and takes piece b mod pieces, so the
-// part of the stream that an XCD's L2 sees is an eighth of it.  No piece shorter than 8 tiles.
+// part of the stream that an XCD's L2 sees is an eighth of it.  No piece shorter than 8 tiles, or than 2 where 8 would
+// leave CUs idle (a tile takes about 1 us, a piece's start and its part of the join about 2).
 int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   if (forced > 0) return static_cast<int32_t>(std::min<int64_t>(forced, tiles));
-  const int64_t most = std::max<int64_t>(1, tiles / 8);
-  int64_t want = up(768, up(own_tiles, kWaves));
+  const int64_t groups = up(own_tiles, kWaves);
+  const int64_t most = std::max<int64_t>(1, groups * (tiles / 8) < 256 ? std::min(up(256, groups), tiles / 2) : tiles / 8);
+  int64_t want = up(768, groups);
   if (most >= 8) want = up(want, 8) * 8;
   return static_cast<int32_t>(std::min({want, most, static_cast<int64_t>(256)}));
 }
@@ -2182,9 +2214,11 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       if (t.entries > 0) {
         for (int q = 0; q < p.passes; ++q, from ^= 1) {
           const dim3 blocks(static_cast<unsigned>(p.sort_blocks));
-          hipLaunchKernelGGL(k_sort_count, blocks, dim3(kThreads), 0, s, rec[from].key, t.entries, q * p.bits, 1 << p.bits, at_i(p.hist),
-                             p.sort_blocks);
-          hipLaunchKernelGGL(k_sort_scan, dim3(1 << p.bits), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
+          if (p.sort_blocks > 1) {
+            hipLaunchKernelGGL(k_sort_count, blocks, dim3(kThreads), 0, s, rec[from].key, t.entries, q * p.bits, 1 << p.bits, at_i(p.hist),
+                               p.sort_blocks);
+            hipLaunchKernelGGL(k_sort_scan, dim3(1 << p.bits), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
+          }
           hipLaunchKernelGGL(k_sort_move, blocks, dim3(kThreads), 0, s, rec[from], rec[from ^ 1], t.entries, q * p.bits, p.bits,
                              at_i(p.hist), p.sort_blocks, at_i(p.bins), p.passes == 1 ? first : nullptr, firsts);
         }
