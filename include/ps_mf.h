@@ -282,6 +282,26 @@ int ps_mf_loss(ps_mf_t *h, double *out);
    several host threads) race.  Synchronizes. */
 int ps_mf_loss_noalloc(ps_mf_t *h, double *out);
 
+/* Softmax loss at the latest version (implicit feedback, the ratings as weights of what a user chose
+   among all items): sum over every loaded rating of D_ij (lse_i - L_i . R_j), lse_i the log-sum-exp of
+   L_i . R_j over all items; users without rating add nothing.  A user's part in fp32, their sum in
+   fp64 in user order.  Runs on the operators of ps_soft.h; the first call lays the ratings out by
+   user, and the workspace is kept until the handle is destroyed.  Synchronizes. */
+int ps_mf_softmax_loss(ps_mf_t *h, double *out);
+
+/* The k items of the largest L_i . R_j at the latest version for n users, 1 <= k <= 256: host arrays
+   items and scores (n x k), by decreasing score, equal ones by increasing item; the order is that of
+   64-bit sums.  users[n] lists the users (any order, repeats allowed; EINVAL for one out of range),
+   NULL: all of them, n = the handle's.  exclude_rated != 0 leaves out the items that the user rated;
+   where fewer than k are left: item -1, score -INFINITY.  Synchronizes. */
+int ps_mf_top_items(ps_mf_t *h, const int32_t *users, int64_t n, int32_t k, int32_t exclude_rated, int32_t *items,
+                    float *scores);
+
+/* Device addresses of the latest version: L (users rows) and R (items rows), K floats each at a row
+   stride of *ld floats, e.g. for the operators of ps_soft.h.  Read only, on the handle's stream (or
+   ordered after it); the next ps_mf_clock, ps_mf_set_factors or ps_mf_destroy ends their use. */
+int ps_mf_device_factors(ps_mf_t *h, const float **L, const float **R, int64_t *ld);
+
 /* Copy the latest committed version into host arrays L (users x K), R (items x K).
    Synchronizes. */
 int ps_mf_get_factors(ps_mf_t *h, float *L, float *R);

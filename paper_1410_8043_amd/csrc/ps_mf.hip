@@ -39,6 +39,7 @@
 #include <vector>
 
 #include "../../include/ps_mf.h"
+#include "../../include/ps_soft.h"
 #include "layout.h"
 
 // The fp64 partial sums of the loss for callers that cannot allocate (ps_mf_loss_noalloc):
@@ -948,6 +949,48 @@ __global__ __launch_bounds__(kSumThreads) void k_sum_partials(const double *__re
     __syncthreads();
   }
   if (threadIdx.x == 0) *out = sh[0];
+}
+
+// k_sum_partials over fp32 values (rows' losses)
+__global__ __launch_bounds__(kSumThreads) void k_sum_rows(const float *__restrict__ row, int64_t n, double *__restrict__ out) {
+  __shared__ double sh[kSumThreads];
+  double s = 0.0;
+#pragma unroll 8
+  for (int64_t x = threadIdx.x; x < n; x += kSumThreads) s += row[x];
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = kSumThreads / 2; o > 0; o >>= 1) {
+    if (static_cast<int>(threadIdx.x) < o) sh[threadIdx.x] += sh[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *out = sh[0];
+}
+
+// One block's lists by user to their places among all blocks' (a wavefront per user)
+__global__ __launch_bounds__(kBlock) void k_copy_lists(int64_t n, const int64_t *__restrict__ from, const int32_t *__restrict__ col,
+                                                       const float *__restrict__ val, const int64_t *__restrict__ to,
+                                                       int32_t *__restrict__ item, float *__restrict__ out) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
+  if (i >= n) return;
+  const int64_t b = from[i], len = from[i + 1] - b, t = to[i];
+  for (int64_t q = threadIdx.x & 63; q < len; q += 64) {
+    item[t + q] = col[b + q];
+    out[t + q] = val[b + q];
+  }
+}
+
+// Some users' factor rows, and the items they rated at ptr[r] .. ptr[r + 1] (a wavefront per user; list NULL: rows only)
+__global__ __launch_bounds__(kBlock) void k_pick_users(int64_t m, const int32_t *__restrict__ users, const float *__restrict__ L, int32_t Kp,
+                                                       float *__restrict__ rows, const int64_t *__restrict__ ptr,
+                                                       const int64_t *__restrict__ from, const int32_t *__restrict__ list,
+                                                       int32_t *__restrict__ out) {
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
+  if (r >= m) return;
+  const int lane = threadIdx.x & 63;
+  for (int k = lane; k < Kp; k += 64) rows[r * Kp + k] = L[static_cast<int64_t>(users[r]) * Kp + k];
+  if (!list) return;
+  const int64_t b = ptr[r], len = ptr[r + 1] - b, f = from[r];
+  for (int64_t q = lane; q < len; q += 64) out[b + q] = list[f + q];
 }
 
 struct FinalArgs {
@@ -2021,6 +2064,17 @@ struct ps_mf {
   double *loss_out = nullptr;  // pinned host memory that the last loss kernel writes
   std::vector<DeviceBlock> dblocks;
   std::vector<void *> allocations;
+  // softmax loss and best items: the operators over all items, the ratings of all blocks by user, and
+  // what their calls need, kept from call to call
+  ps_soft_t *soft = nullptr;
+  std::vector<int64_t> list_ptr;       // [users + 1]
+  const int32_t *list_item = nullptr;  // NULL: not laid out yet
+  const float *list_val = nullptr;
+  struct Buffer {
+    void *p = nullptr;
+    size_t bytes = 0;
+  };
+  Buffer all_ptr, all_item, all_val, row_loss, pick_rows, pick_ptr, pick_item, pick_users, best_item, best_score;
   // timing
   struct Ev {
     int kernel;
@@ -2824,6 +2878,8 @@ int ps_mf_set_owner_map(ps_mf_t *h, const int32_t *owner) {
 
 int ps_mf_set_stream(ps_mf_t *h, void *hip_stream) {
   if (!h) return PS_MF_EINVAL;
+  if (h->soft && h->stream)  // the operators leave the old stream while it lives
+    if (const int r = ps_soft_set_stream(h->soft, nullptr)) return fail(h, r, "%s", ps_soft_last_error(h->soft));
   if (h->stream && h->own_stream) {
     (void)hipStreamSynchronize(h->stream);
     (void)hipStreamDestroy(h->stream);
@@ -3184,6 +3240,165 @@ int scratch_address(ps_mf_t *h, double **out) {
   return PS_MF_OK;
 }
 
+// ---- the operators over all items (ps_soft.h) on the handle's factors and ratings
+
+void latest(const ps_mf_t *h, const float **L, const float **R) {
+  *L = h->ring + (h->clock % (h->s + 1)) * (h->N + h->M) * h->Kp;
+  *R = *L + h->N * h->Kp;
+}
+
+int soft_fail(ps_mf_t *h, int rc) {  // the codes are the same
+  return rc ? fail(h, rc, "%s", ps_soft_last_error(h->soft)) : PS_MF_OK;
+}
+
+int soft_open(ps_mf_t *h) {
+  if (!h->soft) {
+    const int rc = ps_soft_create(h->M, h->K, PS_SOFT_F32, &h->soft);
+    if (rc) return fail(h, rc, "the operators over %lld items of rank %d", (long long)h->M, h->K);
+    if (const int r = ps_soft_set_option(h->soft, PS_SOFT_OPT_DEVICE, h->device)) return soft_fail(h, r);
+  }
+  return soft_fail(h, ps_soft_set_stream(h->soft, h->stream));
+}
+
+int buffer(ps_mf_t *h, ps_mf::Buffer &b, size_t bytes) {
+  if (b.p && b.bytes >= bytes) return PS_MF_OK;
+  HIP_TRY(h, hipStreamSynchronize(h->stream));
+  if (b.p) (void)hipFree(b.p);
+  b = ps_mf::Buffer{};
+  const size_t want = std::max<size_t>(bytes, 256);
+  const hipError_t e = hipMalloc(&b.p, want);
+  if (e != hipSuccess) {
+    b.p = nullptr;
+    (void)hipGetLastError();
+    return fail(h, e == hipErrorOutOfMemory ? PS_MF_ENOMEM : PS_MF_EDEVICE, "hipMalloc(%zu bytes) failed: %s", want, hipGetErrorString(e));
+  }
+  b.bytes = want;
+  return PS_MF_OK;
+}
+
+// Block b's lists to their places `to` among all blocks'; moves `to` behind them
+int merge_block(ps_mf_t *h, int b, std::vector<int64_t> &from, std::vector<int64_t> &to, ps_mf::Buffer &d_from, ps_mf::Buffer &d_to) {
+  const size_t n = static_cast<size_t>(h->N);
+  from[0] = 0;
+  for (size_t i = 0; i < n; ++i) from[i + 1] = from[i] + h->layout[b].ucount[i];
+  int r;
+  if ((r = buffer(h, d_to, n * 8)) || (r = buffer(h, d_from, (n + 1) * 8))) return r;
+  HIP_TRY(h, hipMemcpyAsync(d_to.p, to.data(), n * 8, hipMemcpyHostToDevice, h->stream));
+  HIP_TRY(h, hipMemcpyAsync(d_from.p, from.data(), (n + 1) * 8, hipMemcpyHostToDevice, h->stream));
+  hipLaunchKernelGGL(k_copy_lists, dim3(static_cast<unsigned>((n + 3) / 4)), dim3(kBlock), 0, h->stream, static_cast<int64_t>(n),
+                     static_cast<const int64_t *>(d_from.p), h->dblocks[b].col, h->dblocks[b].val, static_cast<const int64_t *>(d_to.p),
+                     static_cast<int32_t *>(h->all_item.p), static_cast<float *>(h->all_val.p));
+  HIP_TRY(h, hipGetLastError());
+  HIP_TRY(h, hipStreamSynchronize(h->stream));  // the host arrays are free again
+  for (size_t i = 0; i < n; ++i) to[i] += h->layout[b].ucount[i];
+  return PS_MF_OK;
+}
+
+// The ratings by user: one block's lists are that already; several blocks' are copied behind each other
+int lists_by_user(ps_mf_t *h) {
+  if (h->list_item) return PS_MF_OK;
+  const size_t n = static_cast<size_t>(h->N);
+  std::vector<int64_t> ptr(n + 1, 0);
+  for (int b = 0; b < h->B; ++b)
+    for (size_t i = 0; i < n; ++i) ptr[i + 1] += h->layout[b].ucount[i];
+  for (size_t i = 0; i < n; ++i) ptr[i + 1] += ptr[i];
+  int r;
+  if ((r = buffer(h, h->all_ptr, (n + 1) * 8))) return r;
+  HIP_TRY(h, hipMemcpyAsync(h->all_ptr.p, ptr.data(), (n + 1) * 8, hipMemcpyHostToDevice, h->stream));
+  HIP_TRY(h, hipStreamSynchronize(h->stream));
+  if (h->B > 1) {
+    if ((r = buffer(h, h->all_item, static_cast<size_t>(ptr[n]) * 4)) || (r = buffer(h, h->all_val, static_cast<size_t>(ptr[n]) * 4))) return r;
+    std::vector<int64_t> to(ptr.begin(), ptr.end() - 1), from(n + 1);
+    ps_mf::Buffer d_to, d_from;
+    for (int b = 0; b < h->B && !r; ++b)
+      if (h->dblocks[b].nnz) r = merge_block(h, b, from, to, d_from, d_to);
+    if (d_to.p) (void)hipFree(d_to.p);
+    if (d_from.p) (void)hipFree(d_from.p);
+    if (r) return r;
+  }
+  h->list_ptr.swap(ptr);
+  h->list_val = h->B > 1 ? static_cast<const float *>(h->all_val.p) : h->dblocks[0].val;
+  h->list_item = h->B > 1 ? static_cast<const int32_t *>(h->all_item.p) : h->dblocks[0].col;
+  return PS_MF_OK;
+}
+
+constexpr int64_t kSoftRows = 1 << 18;  // users of one call of the loss: their tiles and sums stay near 0.3 GB
+
+int softmax_loss(ps_mf_t *h, double *out) {
+  int r = ensure_device(h);
+  if (r || (r = soft_open(h)) || (r = lists_by_user(h)) || (r = buffer(h, h->row_loss, static_cast<size_t>(h->N) * 4))) return r;
+  const float *L, *R;
+  latest(h, &L, &R);
+  float *loss = static_cast<float *>(h->row_loss.p);
+  for (int64_t i = 0; i < h->N; i += kSoftRows) {
+    const int64_t m = std::min(kSoftRows, h->N - i);
+    r = ps_soft_xent(h->soft, m, L + i * h->Kp, h->Kp, R, h->Kp, static_cast<const int64_t *>(h->all_ptr.p) + i, h->list_item,
+                     h->list_val, h->list_ptr.back(), nullptr, loss + i, nullptr, nullptr, 0, nullptr, 0);
+    if (r) return soft_fail(h, r);
+  }
+  hipLaunchKernelGGL(k_sum_rows, dim3(1), dim3(kSumThreads), 0, h->stream, loss, h->N, h->loss_out);
+  HIP_TRY(h, hipGetLastError());
+  HIP_TRY(h, hipStreamSynchronize(h->stream));
+  *out = *static_cast<volatile double *>(h->loss_out);
+  return PS_MF_OK;
+}
+
+constexpr int64_t kPickRows = 1 << 16;  // users of one call of the search
+
+int top_items(ps_mf_t *h, const int32_t *users, int64_t n, int32_t k, bool exclude, int32_t *items, float *scores) {
+  int r = ensure_device(h);
+  if (r || (r = soft_open(h)) || (exclude && (r = lists_by_user(h)))) return r;
+  const float *L, *R;
+  latest(h, &L, &R);
+  const int64_t most = std::min(n, kPickRows);
+  if ((r = buffer(h, h->best_item, static_cast<size_t>(most * k) * 4)) || (r = buffer(h, h->best_score, static_cast<size_t>(most * k) * 4))) return r;
+  std::vector<int64_t> from, ptr;
+  for (int64_t i = 0; i < n; i += kPickRows) {
+    const int64_t m = std::min(kPickRows, n - i);
+    const float *X = L + i * h->Kp;
+    const int64_t *row_ptr = exclude ? static_cast<const int64_t *>(h->all_ptr.p) + i : nullptr;
+    const int32_t *list = exclude ? h->list_item : nullptr;
+    int64_t entries = exclude ? h->list_ptr.back() : 0;
+    if (users) {  // their rows and lists, in the order asked for
+      const size_t sm = static_cast<size_t>(m);
+      ptr.assign(sm + 1, 0);
+      from.assign(sm, 0);
+      for (size_t q = 0; exclude && q < sm; ++q) {
+        const int32_t u = users[i + static_cast<int64_t>(q)];
+        from[q] = h->list_ptr[u];
+        ptr[q + 1] = ptr[q] + h->list_ptr[u + 1] - from[q];
+      }
+      entries = ptr.back();
+      if (entries > 0x7fffffff - 64) return fail(h, PS_MF_EINVAL, "the users' lists together exceed 2^31 - 65 items");
+      if ((r = buffer(h, h->pick_rows, sm * h->Kp * 4)) || (r = buffer(h, h->pick_ptr, (2 * sm + 1) * 8)) ||
+          (r = buffer(h, h->pick_item, static_cast<size_t>(entries) * 4)) || (r = buffer(h, h->pick_users, sm * 4)))
+        return r;
+      int64_t *d_ptr = static_cast<int64_t *>(h->pick_ptr.p);
+      HIP_TRY(h, hipMemcpyAsync(h->pick_users.p, users + i, sm * 4, hipMemcpyHostToDevice, h->stream));
+      HIP_TRY(h, hipMemcpyAsync(d_ptr, ptr.data(), (sm + 1) * 8, hipMemcpyHostToDevice, h->stream));
+      HIP_TRY(h, hipMemcpyAsync(d_ptr + sm + 1, from.data(), sm * 8, hipMemcpyHostToDevice, h->stream));
+      hipLaunchKernelGGL(k_pick_users, dim3(static_cast<unsigned>((sm + 3) / 4)), dim3(kBlock), 0, h->stream, m,
+                         static_cast<const int32_t *>(h->pick_users.p), L, h->Kp, static_cast<float *>(h->pick_rows.p), d_ptr,
+                         d_ptr + sm + 1, list, static_cast<int32_t *>(h->pick_item.p));
+      HIP_TRY(h, hipGetLastError());
+      X = static_cast<const float *>(h->pick_rows.p);
+      row_ptr = exclude ? d_ptr : nullptr;
+      list = exclude ? static_cast<const int32_t *>(h->pick_item.p) : nullptr;
+    }
+    r = ps_soft_top(h->soft, m, X, h->Kp, R, h->Kp, k, row_ptr, list, entries, static_cast<int32_t *>(h->best_item.p),
+                    static_cast<float *>(h->best_score.p), k);
+    if (r) {
+      soft_fail(h, r);
+      (void)hipStreamSynchronize(h->stream);  // the copies from the host arrays
+      return r;
+    }
+    HIP_TRY(h, hipMemcpyAsync(items + i * k, h->best_item.p, static_cast<size_t>(m * k) * 4, hipMemcpyDeviceToHost, h->stream));
+    HIP_TRY(h, hipMemcpyAsync(scores + i * k, h->best_score.p, static_cast<size_t>(m * k) * 4, hipMemcpyDeviceToHost, h->stream));
+    HIP_TRY(h, hipStreamSynchronize(h->stream));
+  }
+  return PS_MF_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -3252,6 +3467,39 @@ int ps_mf_loss_noalloc(ps_mf_t *h, double *out) {
   double *sc = nullptr;
   if ((r = scratch_address(h, &sc))) return r;
   return loss_into(h, sc, out);
+}
+
+int ps_mf_softmax_loss(ps_mf_t *h, double *out) {
+  if (!h || !out) return PS_MF_EINVAL;
+  if (!h->loaded || !h->has_factors) return fail(h, PS_MF_ESTATE, "load ratings and set factors before the loss");
+  try {
+    return softmax_loss(h, out);
+  } catch (const std::bad_alloc &) {
+    return fail(h, PS_MF_ENOMEM, "host memory for the ratings by user");
+  }
+}
+
+int ps_mf_top_items(ps_mf_t *h, const int32_t *users, int64_t n, int32_t k, int32_t exclude_rated, int32_t *items, float *scores) {
+  if (!h) return PS_MF_EINVAL;
+  if (!h->loaded || !h->has_factors) return fail(h, PS_MF_ESTATE, "load ratings and set factors before asking for items");
+  if (k < 1 || k > 256) return fail(h, PS_MF_EINVAL, "k must be in [1, 256]");
+  if (n < 0 || (n > 0 && (!items || !scores))) return fail(h, PS_MF_EINVAL, "bad output arrays");
+  if (!users && n != h->N) return fail(h, PS_MF_EINVAL, "without a list of users n is their number, %lld", (long long)h->N);
+  for (int64_t r = 0; users && r < n; ++r)
+    if (users[r] < 0 || users[r] >= h->N) return fail(h, PS_MF_EINVAL, "users[%lld] = %d is not in [0, users)", (long long)r, users[r]);
+  try {
+    return top_items(h, users, n, k, exclude_rated != 0, items, scores);
+  } catch (const std::bad_alloc &) {
+    return fail(h, PS_MF_ENOMEM, "host memory for the users' lists");
+  }
+}
+
+int ps_mf_device_factors(ps_mf_t *h, const float **L, const float **R, int64_t *ld) {
+  if (!h || !L || !R || !ld) return PS_MF_EINVAL;
+  if (!h->has_factors) return fail(h, PS_MF_ESTATE, "no factors set");
+  latest(h, L, R);
+  *ld = h->Kp;
+  return PS_MF_OK;
 }
 
 int ps_mf_get_version(ps_mf_t *h, int64_t v, float *L, float *R) {
@@ -3434,6 +3682,10 @@ void ps_mf_destroy(ps_mf_t *h) {
     if (ex) (void)hipGraphExecDestroy(ex);
   for (hipGraphExec_t ex : h->sweep_exec)
     if (ex) (void)hipGraphExecDestroy(ex);
+  ps_soft_destroy(h->soft);
+  for (ps_mf::Buffer *b : {&h->all_ptr, &h->all_item, &h->all_val, &h->row_loss, &h->pick_rows, &h->pick_ptr, &h->pick_item,
+                           &h->pick_users, &h->best_item, &h->best_score})
+    if (b->p) (void)hipFree(b->p);
   for (void *p : h->allocations) (void)hipFree(p);
   if (h->loss_out) (void)hipHostFree(h->loss_out);
   if (h->side_stream) (void)hipStreamDestroy(h->side_stream);

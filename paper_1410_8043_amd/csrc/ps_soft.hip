@@ -29,7 +29,7 @@
 #include <type_traits>
 #include <vector>
 
-#include "ps_soft.h"
+#include "../../include/ps_soft.h"
 
 namespace {
 

@@ -35,7 +35,8 @@ KERNEL_SWEEP, KERNEL_COMMIT = 0, 1
 
 SYMBOLS = ("ps_mf_create", "ps_mf_set_option", "ps_mf_set_value_bound", "ps_mf_set_owner_map", "ps_mf_set_stream",
            "ps_mf_load_ratings",
-           "ps_mf_set_factors", "ps_mf_clock", "ps_mf_loss", "ps_mf_loss_noalloc", "ps_mf_get_factors", "ps_mf_get_version",
+           "ps_mf_set_factors", "ps_mf_clock", "ps_mf_loss", "ps_mf_loss_noalloc", "ps_mf_softmax_loss",
+           "ps_mf_top_items", "ps_mf_device_factors", "ps_mf_get_factors", "ps_mf_get_version",
            "ps_mf_get_clock", "ps_mf_export_index", "ps_mf_kernel_time", "ps_mf_last_error", "ps_mf_destroy")
 
 
@@ -56,6 +57,9 @@ def _load_lib():
         "ps_mf_clock": [vp, i32],
         "ps_mf_loss": [vp, ctypes.POINTER(dbl)],
         "ps_mf_loss_noalloc": [vp, ctypes.POINTER(dbl)],
+        "ps_mf_softmax_loss": [vp, ctypes.POINTER(dbl)],
+        "ps_mf_top_items": [vp, vp, i64, i32, i32, vp, vp],
+        "ps_mf_device_factors": [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(i64)],
         "ps_mf_get_factors": [vp, vp, vp],
         "ps_mf_get_version": [vp, i64, vp, vp],
         "ps_mf_get_clock": [vp, ctypes.POINTER(i64)],
@@ -148,6 +152,42 @@ def ps_mf_loss_noalloc(h):
     out = ctypes.c_double()
     _check(h, "ps_mf_loss_noalloc", _lib.ps_mf_loss_noalloc(h, ctypes.byref(out)))
     return out.value
+
+
+def ps_mf_softmax_loss(h):
+    out = ctypes.c_double()
+    _check(h, "ps_mf_softmax_loss", _lib.ps_mf_softmax_loss(h, ctypes.byref(out)))
+    return out.value
+
+
+def ps_mf_top_items(h, users, n, k, exclude_rated=True):
+    """users: None for all n of them, else a list of n."""
+    if users is not None:
+        users = _arr(users, np.int32)
+        if users.ndim != 1 or users.shape[0] != n:
+            raise ValueError("users must be a list of n")
+    k = int(k)
+    shape = (max(0, int(n)), max(0, k))
+    items, scores = np.empty(shape, np.int32), np.empty(shape, np.float32)
+    _check(h, "ps_mf_top_items", _lib.ps_mf_top_items(h, None if users is None else users.ctypes.data, int(n), k,
+                                                      int(bool(exclude_rated)), items.ctypes.data, scores.ctypes.data))
+    return items, scores
+
+
+def ps_mf_device_factors(h):
+    """Device addresses of L and R and their row stride in floats."""
+    L, R, ld = ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_int64()
+    _check(h, "ps_mf_device_factors", _lib.ps_mf_device_factors(h, ctypes.byref(L), ctypes.byref(R), ctypes.byref(ld)))
+    return L.value, R.value, ld.value
+
+
+class _DeviceRows:
+    """Rows in device memory, for torch.as_tensor; keeps the handle that owns them."""
+
+    def __init__(self, owner, address, rows, K, ld):
+        self.owner = owner
+        self.__cuda_array_interface__ = {"shape": (rows, K), "strides": (4 * ld, 4), "typestr": "<f4", "data": (address, False),
+                                         "version": 2}
 
 
 def ps_mf_get_factors(h, users, items, K):
@@ -286,6 +326,19 @@ class PsMf:
 
     def loss(self):
         return ps_mf_loss(self.h)
+
+    def softmax_loss(self):
+        return ps_mf_softmax_loss(self.h)
+
+    def top_items(self, k, users=None, exclude_rated=True):
+        """The k best items of the users (None: of all) and their scores, without those that the user rated."""
+        return ps_mf_top_items(self.h, users, self.N if users is None else len(users), k, exclude_rated)
+
+    def device_factors(self):
+        """L and R of the latest version as torch tensors in place, on the handle's device.  Read only, ordered after the handle's
+        stream; the next clock, set_factors or close ends their use."""
+        L, R, ld = ps_mf_device_factors(self.h)
+        return (torch.as_tensor(_DeviceRows(self, L, self.N, self.K, ld)), torch.as_tensor(_DeviceRows(self, R, self.M, self.K, ld)))
 
     def get_factors(self):
         return ps_mf_get_factors(self.h, self.N, self.M, self.K)

@@ -122,6 +122,22 @@ def test_binding_refuses_cpu_tensors_and_wrong_shapes():
         h.xent(X, W, item)
 
 
+def test_factorization_calls_refuse_without_factors():
+    from paper_1410_8043_amd import ps_mf
+
+    lib = ps_mf._lib
+    assert lib.ps_mf_softmax_loss(None, ctypes.byref(ctypes.c_double())) == ps_mf.EINVAL
+    assert lib.ps_mf_top_items(None, None, 0, 1, 0, None, None) == ps_mf.EINVAL
+    assert lib.ps_mf_device_factors(None, None, None, None) == ps_mf.EINVAL
+    with ps_mf.PsMf(4, 5, 3, 1, 0, 0.1, 0.0, host_only=True) as g:
+        assert lib.ps_mf_softmax_loss(g.h, None) == ps_mf.EINVAL
+        g.load_ratings(np.array([0, 3]), np.array([1, 2]), np.ones(2))
+        for call in (g.softmax_loss, lambda: g.top_items(2), g.device_factors):
+            with pytest.raises(ps_mf.PsMfError) as e:
+                call()
+            assert e.value.code == ps_mf.ESTATE
+
+
 # ---- the reference against automatic differentiation, and that its bounds mean something
 def torch_loss(x, w, y, extra, weight, tau):
     s = x @ w.T / tau
