@@ -1001,13 +1001,149 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   }
 }
 
+// ------------------------------------------------------------------ scores in 64 bits
+//
+// A score in 64 bits: products of the tables' numbers are exact, and the sum has one order everywhere: 8 lanes of 4
+// numbers each take every eighth 4, then the lanes are added in pairs.
+constexpr int kDotLanes = 8;
+template <int Move>
+__device__ inline double moved(double v) {  // of another lane of the 8: 0xb1 of the pair, 0x4e of the other pair, 0x141 of the other four
+  const unsigned long long u = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), Move, 0xf, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), Move, 0xf, 0xf, false);
+  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo)));
+}
+__device__ inline double sum8(double s) {
+  s += moved<0xb1>(s);
+  s += moved<0x4e>(s);
+  return s + moved<0x141>(s);
+}
+// Of lane l ^ 4: two moves, each for half of the lanes
+__device__ inline int far4(int v) {
+  const int up = __builtin_amdgcn_update_dpp(0, v, 0x104, 0xf, 0x5, false);  // lanes 0..3 and 8..11 of 16 take l + 4
+  return __builtin_amdgcn_update_dpp(up, v, 0x114, 0xf, 0xa, false);         // the others l - 4
+}
+__device__ inline double far4(double v) {
+  const unsigned long long u = __double_as_longlong(v);
+  const uint32_t lo = static_cast<uint32_t>(far4(static_cast<int>(u))), hi = static_cast<uint32_t>(far4(static_cast<int>(u >> 32)));
+  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
+}
+// The sums of R numbers over 8 lanes, sum8's order: lane l gets number spread_of<R>(l), 8 / R lanes each.  Each step halves
+// what a lane holds, so 8 numbers take 7 additions instead of 24
+template <int R>
+__device__ inline int spread_of(int l) {
+  return R == 8 ? (l & 1) << 2 | (l & 2) | l >> 2 : R == 4 ? (l & 1) << 1 | (l >> 1 & 1) : 0;
+}
+template <int R>
+__device__ inline double spread8(double (&s)[R], int l) {
+  static_assert(R == 1 || R == 4 || R == 8, "1, 4 or 8 numbers");
+  if constexpr (R == 1) {
+    return sum8(s[0]);
+  } else {
+    double a[R / 2], b[R / 4];
+    const bool odd = l & 1, second = l & 2, far = l & 4;
+#pragma unroll
+    for (int i = 0; i < R / 2; ++i) {
+      const double keep = odd ? s[R / 2 + i] : s[i], give = odd ? s[i] : s[R / 2 + i];
+      a[i] = keep + moved<0xb1>(give);
+    }
+#pragma unroll
+    for (int i = 0; i < R / 4; ++i) {
+      const double keep = second ? a[R / 4 + i] : a[i], give = second ? a[i] : a[R / 4 + i];
+      b[i] = keep + moved<0x4e>(give);
+    }
+    if constexpr (R == 4) return b[0] + far4(b[0]);
+    else return (far ? b[1] : b[0]) + far4(far ? b[0] : b[1]);
+  }
+}
+template <class T>
+__device__ inline double dot64(const double *x, const T *w, int l, int K, bool vec) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int k = 4 * l; k < K; k += 4 * kDotLanes) {
+    const f32x4 v = load4(w, k, K, vec);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);
+  }
+  return sum8(s);
+}
+
+// ------------------------------------------------------------------ few rows, the loss alone
+//
+// Log-sum-exps of R rows over pieces of the items: scores in 64 bits from the tables as they are (ps_soft_top's), the sums
+// in fp32 with the maximum of what a lane has seen.  Reads W once for R rows; nothing is packed.  Bound by that
+// read and by latency.
+struct FewArgs {
+  int64_t n, own_pad;
+  int32_t items, K;
+  int64_t per;       // items of a piece, a multiple of 32
+  const int32_t *act;
+  float scale;       // log2(e) / tau
+  float *m, *l;      // [pieces][own_pad]
+};
+template <class T, int R>
+__global__ __launch_bounds__(kThreads) void k_few(FewArgs a, Table<T> xt, Table<T> wt) {
+  __shared__ double x[R][kMaxK];
+  __shared__ float part[2][kThreads / 64][R];
+  const int64_t r0 = static_cast<int64_t>(blockIdx.y) * R;
+  const int l = threadIdx.x & (kDotLanes - 1), g = threadIdx.x / kDotLanes;
+  for (int q = threadIdx.x; q < R * a.K; q += kThreads) {
+    const int r = q / a.K, k = q - r * a.K;
+    x[r][k] = r0 + r < a.n && a.act[r0 + r] ? static_cast<double>(to_f(xt.p[(r0 + r) * xt.ld + k])) : 0.0;
+  }
+  for (int q = threadIdx.x; q < R * ((4 - a.K % 4) % 4); q += kThreads) x[q % R][a.K + q / R] = 0.0;  // up to a whole float4
+  __syncthreads();
+  const int row = spread_of<R>(l);
+  const int64_t j0 = blockIdx.x * a.per, j1 = min(j0 + a.per, static_cast<int64_t>(a.items));
+  float top = kNone, sum = 0.f;
+  for (int64_t j = j0 + g; j < j0 + a.per; j += kThreads / kDotLanes) {
+    double s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = 0.0;
+    if (j < j1) {
+      const T *w = wt.p + j * wt.ld;
+#pragma unroll(R == 8 ? 2 : 4)
+      for (int k = 4 * l; k < a.K; k += 4 * kDotLanes) {
+        const f32x4 v = load4(w, k, a.K, wt.vec);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) s[r] = fma(x[r][k + z], static_cast<double>(v[z]), s[r]);
+      }
+    }
+    const float s2 = j < j1 ? static_cast<float>(spread8<R>(s, l) * a.scale) : (static_cast<void>(spread8<R>(s, l)), -__builtin_inff());
+    const float now = fmaxf(top, s2);
+    sum = sum * __builtin_amdgcn_exp2f(top - now) + __builtin_amdgcn_exp2f(s2 - now);
+    top = now;
+  }
+  auto join = [&](float m, float v) {
+    const float now = fmaxf(top, m);
+    sum = sum * __builtin_amdgcn_exp2f(top - now) + v * __builtin_amdgcn_exp2f(m - now);
+    top = now;
+  };
+#pragma unroll
+  for (int o = kDotLanes; o < 64; o <<= 1) join(__shfl_xor(top, o), __shfl_xor(sum, o));
+  if ((threadIdx.x & 63) < R) {
+    part[0][threadIdx.x >> 6][row] = top;
+    part[1][threadIdx.x >> 6][row] = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x < R && r0 + threadIdx.x < a.n) {
+    top = part[0][0][threadIdx.x];
+    sum = part[1][0][threadIdx.x];
+    for (int w = 1; w < kThreads / 64; ++w) join(part[0][w][threadIdx.x], part[1][w][threadIdx.x]);
+    a.m[blockIdx.x * a.own_pad + r0 + threadIdx.x] = top;
+    a.l[blockIdx.x * a.own_pad + r0 + threadIdx.x] = sum * 0x1p7f;  // as the passes' sums: 2^(score - reference + kShift)
+  }
+}
+static_assert(kShift == 7.f, "k_few's sums");
+
 // ------------------------------------------------------------------ the targets by tiles of items
 // A stable sort of the records by their key, up to 10 bits a pass (one pass up to 32,736 items): records of a tile stay
 // in row order, which the pass over rows relies on, and nothing depends on the order of atomics.  A workgroup
 // takes 4096 records, a wavefront 1024 of them in order; the rank of a record among its wavefront's
 // equal digits comes from the lanes' ballots.  Bound by the scattered writes of the payloads.
-constexpr int kBins = 1024, kSortTile = 4096;
-static_assert(kBins == 4 * kThreads, "four digits per thread");
+constexpr int kBins = 1024, kSortTile = 4096, kSortThreads = 512, kSortWaves = kSortThreads / 64;
 
 __global__ __launch_bounds__(kThreads) void k_sort_count(const int32_t *key, int64_t n, int shift, int bins, int32_t *hist, int32_t blocks) {
   __shared__ int32_t cnt[kBins];
@@ -1052,39 +1188,39 @@ struct Records {
   int32_t *key;
   uint2 *pay;
 };
-// first: where the digits start, for the one pass whose digits are the whole keys (NULL otherwise).  A lane's 16 keys and
+// first: where the digits start, for the one pass whose digits are the whole keys (NULL otherwise).  A lane's keys and
 // payloads are read at once: in turn, each round waited for its own (24 us for 4096 records a workgroup, however few)
-__global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out, int64_t n, int shift, int bits, const int32_t *hist,
+__global__ __launch_bounds__(kSortThreads) void k_sort_move(Records in, Records out, int64_t n, int shift, int bits, const int32_t *hist,
                                                         int32_t blocks, const int32_t *total, int64_t *first, int32_t firsts) {
-  constexpr int kOwn = kSortTile / kThreads;
-  __shared__ int32_t cnt[4][kBins], sh[4];
+  constexpr int kOwn = kSortTile / kSortThreads, kDigits = kBins / kSortThreads;  // records and digits of a thread
+  __shared__ int32_t cnt[kSortWaves][kBins], sh[kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << bits;
-  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / 4) + lane;
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kSortTile / kSortWaves) + lane;
   int32_t key[kOwn];
   uint2 pay[kOwn];
 #pragma unroll
   for (int q = 0; q < kOwn; ++q) key[q] = base + 64 * q < n ? in.key[base + 64 * q] : -1;  // keys are not negative
 #pragma unroll
   for (int q = 0; q < kOwn; ++q) pay[q] = base + 64 * q < n ? in.pay[base + 64 * q] : make_uint2(0u, 0u);
-  for (int b = threadIdx.x; b < 4 * kBins; b += kThreads) (&cnt[0][0])[b] = 0;
+  for (int b = threadIdx.x; b < kSortWaves * kBins; b += kSortThreads) (&cnt[0][0])[b] = 0;
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < kOwn; ++q)
     if (key[q] >= 0) atomicAdd(&cnt[wave][(key[q] >> shift) & (bins - 1)], 1);
-  // where each digit starts: the digits before it, four per thread
-  const int b0 = 4 * threadIdx.x;
-  int32_t v[4], at[4], s = 0;
+  // where each digit starts: the digits before it
+  const int b0 = kDigits * threadIdx.x;
+  int32_t v[kDigits], at[kDigits], s = 0;
   if (blocks == 1) {  // one workgroup's counts are the totals
     __syncthreads();
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      v[z] = b0 + z < bins ? cnt[0][b0 + z] + cnt[1][b0 + z] + cnt[2][b0 + z] + cnt[3][b0 + z] : 0;
-      at[z] = 0;
+    for (int z = 0; z < kDigits; ++z) {
+      v[z] = at[z] = 0;
+      for (int w = 0; w < kSortWaves && b0 + z < bins; ++w) v[z] += cnt[w][b0 + z];
       s += v[z];
     }
   } else {
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
+    for (int z = 0; z < kDigits; ++z) {
       v[z] = b0 + z < bins ? total[b0 + z] : 0;
       at[z] = b0 + z < bins ? hist[static_cast<int64_t>(b0 + z) * blocks + blockIdx.x] : 0;
       s += v[z];
@@ -1101,12 +1237,12 @@ __global__ __launch_bounds__(kThreads) void k_sort_move(Records in, Records out,
   int32_t before = s - own;
   for (int w = 0; w < wave; ++w) before += sh[w];
 #pragma unroll
-  for (int z = 0; z < 4; ++z) {
+  for (int z = 0; z < kDigits; ++z) {
     if (b0 + z < bins) {
       if (first && blockIdx.x == 0 && b0 + z < firsts) first[b0 + z] = before;
       int32_t to = before + at[z];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < kSortWaves; ++w) {
         const int32_t c = cnt[w][b0 + z];
         cnt[w][b0 + z] = to;
         to += c;
@@ -1259,71 +1395,6 @@ __device__ inline void best_add(Best b, int k, bool want, uint64_t key, int32_t 
     least = now > least ? now : least;
   }
   __syncthreads();
-}
-
-// A score in 64 bits: products of the tables' numbers are exact, and the sum has one order everywhere: 8 lanes of 4
-// numbers each take every eighth 4, then the lanes are added in pairs.
-constexpr int kDotLanes = 8;
-template <int Move>
-__device__ inline double moved(double v) {  // of another lane of the 8: 0xb1 of the pair, 0x4e of the other pair, 0x141 of the other four
-  const unsigned long long u = __double_as_longlong(v);
-  const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), Move, 0xf, 0xf, false);
-  const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), Move, 0xf, 0xf, false);
-  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo)));
-}
-__device__ inline double sum8(double s) {
-  s += moved<0xb1>(s);
-  s += moved<0x4e>(s);
-  return s + moved<0x141>(s);
-}
-// Of lane l ^ 4: two moves, each for half of the lanes
-__device__ inline int far4(int v) {
-  const int up = __builtin_amdgcn_update_dpp(0, v, 0x104, 0xf, 0x5, false);  // lanes 0..3 and 8..11 of 16 take l + 4
-  return __builtin_amdgcn_update_dpp(up, v, 0x114, 0xf, 0xa, false);         // the others l - 4
-}
-__device__ inline double far4(double v) {
-  const unsigned long long u = __double_as_longlong(v);
-  const uint32_t lo = static_cast<uint32_t>(far4(static_cast<int>(u))), hi = static_cast<uint32_t>(far4(static_cast<int>(u >> 32)));
-  return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
-}
-// The sums of R numbers over 8 lanes, sum8's order: lane l gets number spread_of<R>(l), 8 / R lanes each.  Each step halves
-// what a lane holds, so 8 numbers take 7 additions instead of 24
-template <int R>
-__device__ inline int spread_of(int l) {
-  return R == 8 ? (l & 1) << 2 | (l & 2) | l >> 2 : R == 4 ? (l & 1) << 1 | (l >> 1 & 1) : 0;
-}
-template <int R>
-__device__ inline double spread8(double (&s)[R], int l) {
-  static_assert(R == 1 || R == 4 || R == 8, "1, 4 or 8 numbers");
-  if constexpr (R == 1) {
-    return sum8(s[0]);
-  } else {
-    double a[R / 2], b[R / 4];
-    const bool odd = l & 1, second = l & 2, far = l & 4;
-#pragma unroll
-    for (int i = 0; i < R / 2; ++i) {
-      const double keep = odd ? s[R / 2 + i] : s[i], give = odd ? s[i] : s[R / 2 + i];
-      a[i] = keep + moved<0xb1>(give);
-    }
-#pragma unroll
-    for (int i = 0; i < R / 4; ++i) {
-      const double keep = second ? a[R / 4 + i] : a[i], give = second ? a[i] : a[R / 4 + i];
-      b[i] = keep + moved<0x4e>(give);
-    }
-    if constexpr (R == 4) return b[0] + far4(b[0]);
-    else return (far ? b[1] : b[0]) + far4(far ? b[0] : b[1]);
-  }
-}
-template <class T>
-__device__ inline double dot64(const double *x, const T *w, int l, int K, bool vec) {
-  double s = 0.0;
-#pragma unroll 4
-  for (int k = 4 * l; k < K; k += 4 * kDotLanes) {
-    const f32x4 v = load4(w, k, K, vec);
-#pragma unroll
-    for (int z = 0; z < 4; ++z) s = fma(x[k + z], static_cast<double>(v[z]), s);
-  }
-  return sum8(s);
 }
 
 template <class T>
@@ -1994,6 +2065,8 @@ bool aligned4(const T *p, int64_t ld) {
 struct Plan {
   int32_t np, k16, kd;
   int64_t n, entries, xt, wt;  // rows, entries, tiles of each table
+  bool few;                    // the loss alone of few rows: k_few instead of the packed tables and the pass
+  int64_t few_items;           // of a piece
   bool want_dx, want_dw;
   int64_t x_stride, w_stride;  // halves per tile
   int32_t rsplits, csplits;
@@ -2023,6 +2096,8 @@ int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   return static_cast<int32_t>(std::min({want, most, static_cast<int64_t>(256)}));
 }
 
+int64_t few_rows(int64_t n) { return n >= 8 ? 8 : n >= 3 ? 4 : 1; }  // that share a read of W
+
 Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   Plan p{};
   p.np = h->type == PS_SOFT_F32 ? 2 : 1;
@@ -2039,6 +2114,15 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   p.rsplits = pieces(p.xt, p.wt, h->splits);
   p.rper = up(p.wt, p.rsplits);
   p.rsplits = static_cast<int32_t>(up(p.wt, p.rper));
+  // in us: packing and the pass take about 12 and the packing's bytes.  One user, 17,770 items, K = 128: 32 -> 24
+  const double scores = static_cast<double>(n) * static_cast<double>(h->items);
+  p.few = !dx && !dw && h->splits == 0 && scores * (5 + 0.065 * h->K) * 1e-6 < 12 + h->items * 4e-6 * h->K;
+  if (p.few) {
+    const int64_t rows = up(std::max<int64_t>(n, 1), few_rows(n)), most = up(h->items, kTopGroup);
+    p.few_items = up(h->items, std::min<int64_t>(most, up(1024, rows)));
+    p.few_items = up(p.few_items, 32) * 32;
+    p.rsplits = static_cast<int32_t>(up(h->items, p.few_items));
+  }
   p.csplits = 0;
   p.cper = 1;
   if (dw) {
@@ -2065,8 +2149,8 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   p.row_part = a.take(kRowParts * 4);
   p.part = a.take(2 * kParts * 4);
   p.scal = a.take(sizeof(Scal));
-  p.px = a.take(p.xt * p.x_stride * 2);
-  p.pw = a.take(p.wt * p.w_stride * 2);
+  p.px = a.take(p.few ? 0 : p.xt * p.x_stride * 2);
+  p.pw = a.take(p.few ? 0 : p.wt * p.w_stride * 2);
   const int64_t rpad = p.rsplits * p.xt * kTile, cpad = p.csplits * p.wt * kTile;
   p.m = a.take(std::max(rpad, cpad) * 4);
   p.l = a.take(rpad * 4);
@@ -2166,26 +2250,35 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       hipLaunchKernelGGL(k_fill_keys, dim3(blocks_for(t.entries, kThreads * 4, 4096)), dim3(kThreads), 0, s, t.key, t.entries, t.dead);
     const unsigned row_blocks = blocks_for(t.n, 4, kRowParts);
     hipLaunchKernelGGL((k_targets<Distill>), dim3(row_blocks), dim3(kThreads), 0, s, t);
-    hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kScanThreads), 0, s, x, w, h->K, row_lanes(h->K), at_f(p.part));
-    const PackSide sx{px, p.x_stride, static_cast<int32_t>(p.xt), dw}, sw{pw, p.w_stride, static_cast<int32_t>(p.wt), dx};
-    hipLaunchKernelGGL((k_pack<T, NP>), dim3(static_cast<unsigned>(p.xt + p.wt)), dim3(kThreads),
-                       static_cast<unsigned>(kTile * (std::min(p.kd, kPackBlocks) * 32 + 1) * 4), s, x, w, sx, sw, h->K, p.k16, p.kd, at_f(p.part),
-                       at_f(p.row_part), static_cast<int32_t>(row_blocks), scal);
     PassArgs a{};
-    a.own = px;
-    a.own_stride = p.x_stride;
-    a.own_tiles = p.xt;
-    a.splits = p.rsplits;
-    a.str = pw;
-    a.str_stride = p.w_stride;
-    a.str_rows = h->items;
-    a.scal = scal;
-    a.scale = scale;
-    a.tiles_per_split = p.rper;
     a.m = at_f(p.m);
     a.l = at_f(p.l);
     a.o = at_f(p.o);
-    run_pass<NP>(a, p.k16, false, dx, s);
+    if (p.few) {
+      const FewArgs f{t.n, p.xt * kTile, t.items, h->K, p.few_items, t.act, scale, a.m, a.l};
+      const int64_t at_once = few_rows(t.n);
+      const dim3 grid(static_cast<unsigned>(p.rsplits), static_cast<unsigned>(up(t.n, at_once)));
+      if (at_once == 8) hipLaunchKernelGGL((k_few<T, 8>), grid, dim3(kThreads), 0, s, f, x, w);
+      else if (at_once == 4) hipLaunchKernelGGL((k_few<T, 4>), grid, dim3(kThreads), 0, s, f, x, w);
+      else hipLaunchKernelGGL((k_few<T, 1>), grid, dim3(kThreads), 0, s, f, x, w);
+    } else {
+      hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kScanThreads), 0, s, x, w, h->K, row_lanes(h->K), at_f(p.part));
+      const PackSide sx{px, p.x_stride, static_cast<int32_t>(p.xt), dw}, sw{pw, p.w_stride, static_cast<int32_t>(p.wt), dx};
+      hipLaunchKernelGGL((k_pack<T, NP>), dim3(static_cast<unsigned>(p.xt + p.wt)), dim3(kThreads),
+                         static_cast<unsigned>(kTile * (std::min(p.kd, kPackBlocks) * 32 + 1) * 4), s, x, w, sx, sw, h->K, p.k16, p.kd, at_f(p.part),
+                         at_f(p.row_part), static_cast<int32_t>(row_blocks), scal);
+      a.own = px;
+      a.own_stride = p.x_stride;
+      a.own_tiles = p.xt;
+      a.splits = p.rsplits;
+      a.str = pw;
+      a.str_stride = p.w_stride;
+      a.str_rows = h->items;
+      a.scal = scal;
+      a.scale = scale;
+      a.tiles_per_split = p.rper;
+      run_pass<NP>(a, p.k16, false, dx, s);
+    }
     RowArgs<T> r{};
     r.t = t;
     r.own_pad = p.xt * kTile;
@@ -2219,7 +2312,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
                                p.sort_blocks);
             hipLaunchKernelGGL(k_sort_scan, dim3(1 << p.bits), dim3(kThreads), 0, s, at_i(p.hist), p.sort_blocks, at_i(p.bins));
           }
-          hipLaunchKernelGGL(k_sort_move, blocks, dim3(kThreads), 0, s, rec[from], rec[from ^ 1], t.entries, q * p.bits, p.bits,
+          hipLaunchKernelGGL(k_sort_move, blocks, dim3(kSortThreads), 0, s, rec[from], rec[from ^ 1], t.entries, q * p.bits, p.bits,
                              at_i(p.hist), p.sort_blocks, at_i(p.bins), p.passes == 1 ? first : nullptr, firsts);
         }
         if (p.passes > 1)

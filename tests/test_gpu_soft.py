@@ -266,6 +266,29 @@ def test_top_forms_agree(soft):
         assert same(x, y) and same(x, z)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n,M,K", [(1, 1, 1), (1, 17_770, 128), (2, 70, 33), (3, 999, 7), (9, 5000, 100), (17, 64, 512), (40, 2049, 50)])
+def test_loss_alone_of_few_rows(soft, n, M, K, dtype):
+    g = gen(24, n, M, K)
+    X, W = tables(n, M, K, dtype, g, 3.0)
+    ptr, item = lists(n, M, 5, g)
+    weight = torch.ones(n)
+    if n > 8:
+        weight[5] = 0
+        X[5] = float("nan")
+        X[6] = X[6] * 100  # one item takes all
+    Xr = torch.where(X.isnan(), torch.zeros_like(X), X)
+    want, bounds = soft_ref.xent(Xr, W, item, ptr, weight=weight.cuda())
+    say(f"few rows n={n} M={M} K={K} {dtype}")
+    with soft.PsSoft(M, K, dtype) as h:
+        got = h.xent(X, W, item, row_ptr=ptr, weight=weight.cuda(), grad=False)
+        assert same(got, h.xent(X, W, item, row_ptr=ptr, weight=weight.cuda(), grad=False))
+        Wn = W.clone()
+        Wn[M // 2, K - 1] = float("nan")
+        assert h.xent(Xr, Wn, item, row_ptr=ptr, grad=False)[1].isnan().all()
+    check("few", got, want, bounds, dtype)
+
+
 def test_equal_calls_give_equal_bits(soft):
     # several tiles and pieces, enough workgroups that their order differs from call to call
     g = gen(23)
