@@ -15,7 +15,7 @@
 // so that its largest number lies in [2^13, 2^14) and is held as one plane of fp16 (bf16 and
 // f16 tables: exact for all numbers above 2^-28 of the largest) or as two, h = fp16(x), l =
 // fp16(x - h) (f32 tables: 22 bits, to 2^-38 of the largest below that), and products drop l*l
-// (2^-22).  The weights p' are held in two planes in both cases.  Sums over items and rows, running
+// (2^-22).  The weights p' are held in two planes too, except in the pass over the rows of 16-bit tables.  Sums over items and rows, running
 // maxima and log-sum-exps are fp32.
 #include <hip/hip_runtime.h>
 
@@ -519,6 +519,11 @@ template <int NP, int KC, int DB, bool COL>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
   constexpr int KD = KC / 2;
+  // Items of 16-bit tables: the weights are the differences (a p - the targets') themselves, so one plane rounds each by
+  // 2^-12 of itself, an eighth of what the gradient's own rounding to bf16 does (fp16: as much), and a third of the
+  // pass's instructions goes.  Rows' weights are p alone, and the targets come off later: one plane would leave
+  // 2^-12 of p where p nearly equals the target, so they have two.
+  constexpr bool one_plane = COL && NP == 1;
   extern __shared__ _Float16 buf[];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -770,10 +775,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       for (int i = 0; i < TA && i < 2 * DB; ++i) read_turned(g[i], t, i);
       u32x4 ph[2], pl[2];
       auto make_planes = [&](int k, int i) {
-        uint32_t h, l;
-        planes(p[8 * k + 2 * i], p[8 * k + 2 * i + 1], h, l);
-        ph[k][i] = h;
-        pl[k][i] = l;
+        if constexpr (one_plane) {
+          ph[k][i] = to_halves(p[8 * k + 2 * i], p[8 * k + 2 * i + 1]);
+        } else {
+          uint32_t h, l;
+          planes(p[8 * k + 2 * i], p[8 * k + 2 * i + 1], h, l);
+          ph[k][i] = h;
+          pl[k][i] = l;
+        }
       };
 #pragma unroll
       for (int i = 0; i < 4; ++i) make_planes(0, i);
@@ -790,7 +799,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           for (int z = 2 * i / DB + 1; z <= 2 * (i + 1) / DB && z < 4; ++z) v[z] = row_values(t + 1, z, 0);
         }
         o[b] = mfma(g[i][0], halves(ph[k]), o[b]);
-        o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
+        if constexpr (!one_plane) o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
         if constexpr (NP == 2) o[b] = mfma(g[i][1], halves(ph[k]), o[b]);
         if (k == 0) {
 #pragma unroll
@@ -875,13 +884,17 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     return;
   }
   const bool act = a.t.act[i];
-  float top = kNone;
-  for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, a.m[s * a.own_pad + i]);
+  float top = kNone, den = 0.f;
+#pragma unroll 4
+  for (int s = lane; s < a.splits; s += 64) {
+    const float m = a.m[s * a.own_pad + i], l = a.l[s * a.own_pad + i];
+    const float now = fmaxf(top, m);
+    den = den * __builtin_amdgcn_exp2f(top - now) + l * __builtin_amdgcn_exp2f(m - now);
+    top = now;
+  }
+  const float mine = top;
   top = wave_max(top);
-  float den = 0.f;
-  for (int s = lane; s < a.splits; s += 64)
-    den += a.l[s * a.own_pad + i] * __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
-  den = wave_sum(den);
+  den = wave_sum(den * __builtin_amdgcn_exp2f(mine - top));
   const float lse2 = top - kShift + log2f(den);
   const float lse = lse2 * 0.69314718055994530942f;
   f32x4 acc[V], o[V];

@@ -6,6 +6,8 @@ Bounds, per value, u = 2^-24 half a step of fp32:
     22 bits (three products dropped or rounded at 2^-22 each make 12 u), and the scaling;
   * a weight exp(s - lse) is off by that of s and of lse, and 2^-20 of the exponential and of its two
     planes of 22 bits; a sum of M of them adds (M + 64) u;
+  * tables of 16 bits: the item gradients' weights g (V p - y) are held in one fp16 number each, off by half a step,
+    2^-11 of themselves (2^-25 of the largest share below 2^-14 of it, within the 2^-34 of the shares' sums below);
   * what is rounded to the tables' type adds half a step of it, and half its smallest step.
 """
 import numpy as np
@@ -34,7 +36,7 @@ def lists_of(item, row_ptr, n, M):
     return rows[keep], at[keep], item[at[keep]]
 
 
-def dense_loss(x, w, y, extra, live, weight, tau):
+def dense_loss(x, w, y, extra, live, weight, tau, halves=False):
     """Losses, log-sum-exps, gradients of weighted rows with target weights y (n x M), and their bounds."""
     n, K = x.shape
     M = w.shape[0]
@@ -66,6 +68,8 @@ def dense_loss(x, w, y, extra, live, weight, tau):
     exact = np.abs(g)[:, None] * np.abs(y) * (max(n, 1) + M + 16) * U
     eX = (big + exact) @ np.abs(w) + 2.0 ** -34 * np.abs(g * V)[:, None] * np.abs(w).max()
     eW = (big + exact).T @ np.abs(x) + 2.0 ** -34 * np.abs(g * V).max(initial=0.0) * np.abs(x).max(initial=0.0)
+    if halves:
+        eW = eW + 2.0 ** -11 * (np.abs(dS) + big + exact).T @ np.abs(x) + 2.0 ** -32 * np.abs(g).max(initial=0.0) * Va.max(initial=0.0) * np.abs(x).sum(0)
     return (loss, lse, dX, dW), (eloss, elog, eX, eW)
 
 
@@ -79,7 +83,7 @@ def xent(X, W, item, row_ptr=None, value=None, weight=None):
     live = np.zeros(n, bool)
     live[rows] = True
     wt = np.ones(n) if weight is None else f64(weight)
-    return dense_loss(x, w, y, np.zeros(n), live, wt, 1.0)
+    return dense_loss(x, w, y, np.zeros(n), live, wt, 1.0, X.dtype != torch.float32)
 
 
 def distill(X, W, item, score, tau, tlse=None, weight=None):
@@ -104,7 +108,7 @@ def distill(X, W, item, score, tau, tlse=None, weight=None):
     r, c = np.nonzero(here)
     np.add.at(y, (r, it[r, c]), q[r, c])
     wt = np.ones(n) if weight is None else f64(weight)
-    vals, errs = dense_loss(x, w, y, extra, live, wt, tau)
+    vals, errs = dense_loss(x, w, y, extra, live, wt, tau, X.dtype != torch.float32)
     # q itself comes from fp32: each is off by eq of itself, t and z up to 4 u of themselves
     live = live & (wt != 0)
     eq = 2.0 ** -20 + 8 * U * (np.abs(np.where(here, t, 0.0)).max(1) + np.abs(np.where(live, z[:, 0], 0.0)))
