@@ -467,6 +467,7 @@ __host__ __device__ constexpr Stage stage_of(int np, int kc, int db, bool col) {
 struct Window {
   const uint2 *pay;
   int at, end, pos;
+  uint32_t due;  // the next record's row
   uint2 now, next[2];
   // a record behind the last: a row above all
   __device__ uint2 get(int i) const { return i < end ? pay[i] : make_uint2(0xffffffffu, 0u); }
@@ -478,6 +479,7 @@ struct Window {
     now = get(at);
     next[0] = get(at + 64);
     next[1] = get(at + 128);
+    due = __builtin_amdgcn_readfirstlane(now.x) >> 5;
   }
   __device__ void step() {
     at += 64;
@@ -485,6 +487,11 @@ struct Window {
     now = next[0];
     next[0] = next[1];
     next[1] = get(at + 128);
+  }
+  __device__ void skip(int n) {  // n records are done
+    pos += n;
+    if (pos == 64) step();
+    due = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(now.x), pos)) >> 5;
   }
 };
 
@@ -586,7 +593,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       const int64_t b = first_of_row(a.pay, a.first[own_tile], a.first[own_tile + 1], static_cast<uint32_t>(t0) * kTile, lane);
       const int64_t e = a.first[own_tile + 1];
       win.open(a.pay, b, e, lane);
-      targets = __any((win.now.x >> 5) < static_cast<uint32_t>(t1) * kTile);
+      targets = win.due < static_cast<uint32_t>(t1) * kTile;
     }
     if (targets) {
       ref = -kLag;
@@ -731,7 +738,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       fetch_scores(t + 2);
     }
     if constexpr (DB > 0) {
-      if (COL && targets) {
+      if (COL && targets && win.due < static_cast<uint32_t>(t + 1) * kTile) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           // this half tile's records, through the wavefront's own table of 32 items x 16 rows in LDS, zero between uses.  A
@@ -739,18 +746,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           // instructions and, within one, in an order that its addresses alone decide.
           const uint32_t limit = static_cast<uint32_t>(t * kTile + 16 * k + 16);
           bool some = false;
-          for (;;) {
+          while (win.due < limit) {
             const bool mine = lane >= win.pos && (win.now.x >> 5) < limit;
             const int n = __popcll(__ballot(mine));
-            if (n == 0) break;
             some = true;
             if (mine) {
               const uint32_t r = (win.now.x >> 5) & 15, c = win.now.x & 31;
               atomicAdd(y + c * 16 + (((r >> 2) ^ ((c >> 2) & 3)) << 2) + (r & 3), __uint_as_float(win.now.y) * unit);
             }
-            win.pos += n;
-            if (win.pos < 64) break;
-            win.step();
+            win.skip(n);
           }
           if (some) {
             __builtin_amdgcn_wave_barrier();
@@ -2103,6 +2107,9 @@ int32_t padded_chunks(int32_t K) {
 int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   if (forced > 0) return static_cast<int32_t>(std::min<int64_t>(forced, tiles));
   const int64_t groups = up(own_tiles, kWaves);
+  // many own rows: a piece more costs its part of the join (782 workgroups of 100,000 items: 8 pieces 1292 us and 190 of
+  // joining, 4 pieces 1274 and 95, 2 pieces 1387 and 48)
+  if (groups >= 512) return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(tiles / 8, groups >= 4096 ? 1 : groups >= 2048 ? 2 : 4)));
   const int64_t most = std::max<int64_t>(1, groups * (tiles / 8) < 256 ? std::min(up(256, groups), tiles / 2) : tiles / 8);
   int64_t want = up(768, groups);
   if (most >= 8) want = up(want, 8) * 8;
