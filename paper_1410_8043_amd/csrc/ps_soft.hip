@@ -1434,15 +1434,17 @@ struct TopArgs {
   int64_t ldo;
 };
 
-// 256 scores, an item per thread: 8 lanes make 8 items' in turn.  item_of(q): the q-th item or -1
+// Up to 256 scores, an item per thread: 8 lanes make 8 items' in turn, the 32 groups of lanes neighbouring ones (80
+// candidates take 3 turns).  item_of(q): the q-th of n, or -1
 template <class T, class F>
-__device__ inline void top_batch(const TopArgs<T> &a, const double *x, Best b, uint64_t &least, F item_of) {
-  const int l = threadIdx.x & (kDotLanes - 1), first = threadIdx.x & ~(kDotLanes - 1);
+__device__ inline void top_batch(const TopArgs<T> &a, const double *x, Best b, uint64_t &least, int n, F item_of) {
+  const int l = threadIdx.x & (kDotLanes - 1), g = threadIdx.x / kDotLanes;
   int32_t mine = -1;
   uint64_t key = 0;
-#pragma unroll 2
+#pragma unroll 4
   for (int q = 0; q < kDotLanes; ++q) {
-    const int32_t j = item_of(first + q);
+    const int at = q * (kThreads / kDotLanes) + g;
+    const int32_t j = at < n ? item_of(at) : -1;
     if (j < 0) continue;  // the same for the 8 lanes
     const double s = dot64(x, a.w.p + j * a.w.ld, l, a.K, a.w.vec);
     if (l == q) {
@@ -1465,7 +1467,7 @@ template <class T>
 __device__ inline void top_all(const TopArgs<T> &a, int64_t r, const double *x, Best b, int64_t j0, int64_t j1) {
   uint64_t least = 0;
   for (int64_t base = j0; base < j1; base += kThreads)
-    top_batch(a, x, b, least, [&](int q) {
+    top_batch(a, x, b, least, kThreads, [&](int q) {
       const int64_t j = base + q;
       if (j >= j1 || (a.excluded && ((a.excluded[r * a.words + (j >> 5)] >> (j & 31)) & 1))) return -1;
       return static_cast<int32_t>(j);
@@ -1731,7 +1733,8 @@ struct ScoreArgs {
   int64_t rows, own_tiles, tiles, steps_per_split;
   int32_t items, splits, words, last;  // last: the chunk of the bound's number
   const uint32_t *excluded;
-  float *most;        // [rows][4 steps] first pass: largest lower bounds
+  float *most;        // [rows][per_row] first pass: largest lower bounds, 4 per step
+  int64_t per_row;
   int64_t steps;
   const float *least; // [rows] second pass: T
   int32_t *found, *count;
@@ -1785,6 +1788,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
         to[u][z] = a.excluded && row[u] >= 0 && t < a.words ? a.excluded[row[u] * a.words + t] : 0u;
       }
   };
+  float even[2][kScoreTiles];  // an even step's bounds (pieces start at even steps)
   if (s0 < s1) {
     fetch(s0, 0);
     read_bits(coming, s0);
@@ -1824,7 +1828,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         if constexpr (!Find) {
-          if (a.excluded) {
+          if (__any(out[u])) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int bit = 8 * (r >> 2) + (r & 3);
@@ -1872,23 +1876,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
       }
     }
     if constexpr (!Find) {
-      static_assert(kScoreTiles == 2, "stored as pairs");
+      // two steps' bounds in one store: the rows lie far apart, each store is a line of its own
+      static_assert(kScoreTiles == 2, "stored as two pairs");
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (row[u] >= 0)
-          *reinterpret_cast<float2 *>(a.most + (row[u] * a.steps + st) * 4 + half * 2) = make_float2(most[u][0], most[u][1]);
+      for (int u = 0; u < 2; ++u) {
+        if (!(st & 1)) {
+          even[u][0] = most[u][0];
+          even[u][1] = most[u][1];
+        }
+        if (row[u] >= 0 && ((st & 1) || st + 1 == s1)) {
+          const float none = -__builtin_inff();
+          *reinterpret_cast<f32x4 *>(a.most + row[u] * a.per_row + (st >> 1) * 8 + half * 4) =
+              f32x4{even[u][0], even[u][1], st & 1 ? most[u][0] : none, st & 1 ? most[u][1] : none};
+        }
+      }
     }
   }
   if constexpr (Find) {
     __syncthreads();
-    for (int m = wave * 64; m < wave * 64 + 64; ++m) {  // a row's list to the others' of its row
-      const int64_t r = own_tile * kTile + (m & 63);
-      const int n = min(have[m], kRowRoom);
-      if (r >= a.rows || n == 0) continue;
-      int to = 0;
-      if (lane == 0) to = atomicAdd(&a.count[r], n);
-      to = __shfl(to, 0);
-      if (lane < n && to + lane < kCandidates) a.found[r * kCandidates + to + lane] = list[m * kRowRoom + lane];
+    // a row's list behind the others' of its row, a lane per row (a row in turn waited for its counter 64 times)
+    const int mine = wave * 64 + lane;
+    const int64_t r = own_tile * kTile + lane;
+    const int n = r < a.rows ? min(have[mine], kRowRoom) : 0;
+    if (n > 0) {
+      const int to = atomicAdd(&a.count[r], n);
+      for (int q = 0; q < n && to + q < kCandidates; ++q) a.found[r * kCandidates + to + q] = list[mine * kRowRoom + q];
     }
   }
 }
@@ -1922,7 +1934,7 @@ __global__ __launch_bounds__(kThreads) void k_top_rank(TopArgs<T> a) {
   } else {
     uint64_t least = 0;
     for (int base = 0; base < n; base += kThreads)
-      top_batch(a, x, b, least, [&](int q) { return base + q < n ? a.found[r * a.room + base + q] : -1; });
+      top_batch(a, x, b, least, n - base, [&](int q) { return a.found[r * a.room + base + q]; });
     best_cut(b, a.k);
   }
   top_out(a, r, b);
@@ -2385,7 +2397,7 @@ struct TopPlan {
   bool filter;
   int64_t rows;  // rows of one launch: what they need stays near a gigabyte
   int32_t words, kc, groups;
-  int64_t xt, wt, steps, per_split;
+  int64_t xt, wt, steps, per_split, per_row;
   int32_t splits;
   int64_t bits, key, maxima, part, px, pw, most, least, found, count, bytes;
 };
@@ -2403,7 +2415,8 @@ TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
   TopPlan p{};
   const int64_t all = std::max<int64_t>(n, 1);
   p.words = static_cast<int32_t>(up(h->items, 32));
-  p.filter = top_by_candidates(all, h->items, h->K);
+  // a threshold needs more groups of 16 items than k: 64 k items leave about k / 8 candidates more than k
+  p.filter = h->items >= 64LL * k && top_by_candidates(all, h->items, h->K);
   if (h->search >= 0) p.filter = h->search == 1;
   p.filter = p.filter && h->items < 1 << 30;  // counts of candidates
   Arena a;
@@ -2411,16 +2424,19 @@ TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
     p.kc = score_chunks(h->K);
     p.wt = up(h->items, kTile);
     p.steps = up(p.wt, kScoreTiles);
-    const int64_t per_row = (exclude ? p.words * 4LL : 0) + p.steps * 16 + kCandidates * 4 + (p.kc + 1) * 32;
+    const int64_t per_row = (exclude ? p.words * 4LL : 0) + p.steps * 16 + 32 + kCandidates * 4 + (p.kc + 1) * 32;
     p.rows = std::min(all, std::max<int64_t>(256, (1LL << 30) / per_row / 256 * 256));
     p.xt = up(p.rows, kTile);
-    p.splits = pieces(up(p.xt, 2), p.steps, h->splits);
-    p.per_split = up(p.steps, p.splits);
+    // two workgroups a CU at once: 512, as multiples of 8 pieces (one XCD's L2 sees its eighth of the items)
+    const int64_t groups = up(p.xt, 2 * kWaves), want = std::max<int64_t>(1, 512 / groups);
+    p.splits = static_cast<int32_t>(std::min<int64_t>(p.steps, h->splits > 0 ? h->splits : want >= 8 ? want / 8 * 8 : want));
+    p.per_split = up(up(p.steps, p.splits), 2) * 2;
     p.splits = static_cast<int32_t>(up(p.steps, p.per_split));
+    p.per_row = up(p.steps, 2) * 8;
     p.part = a.take(2 * kParts * 4);
     p.px = a.take(p.xt * (p.kc + 1) * kFrag * 2);
     p.pw = a.take(p.wt * p.kc * kFrag * 2);
-    p.most = a.take(p.rows * p.steps * 16);
+    p.most = a.take(p.rows * p.per_row * 4);
     p.least = a.take(p.rows * 4);
     p.found = a.take(p.rows * kCandidates * 4);
     p.count = a.take(p.rows * 4);
@@ -2527,12 +2543,13 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
     q.excluded = a.excluded;
     q.most = reinterpret_cast<float *>(base + p.most);
     q.steps = p.steps;
+    q.per_row = p.per_row;
     float *least = reinterpret_cast<float *>(base + p.least);
     q.least = least;
     q.found = reinterpret_cast<int32_t *>(base + p.found);
     q.count = count;
     run_score<false>(q, p.kc, s);
-    hipLaunchKernelGGL(k_top_least, dim3(rows), dim3(kThreads), 0, s, q.most, p.steps * 4, k, least);
+    hipLaunchKernelGGL(k_top_least, dim3(rows), dim3(kThreads), 0, s, q.most, p.per_row, k, least);
     run_score<true>(q, p.kc, s);
     hipLaunchKernelGGL((k_top_rank<T>), dim3(rows), dim3(kThreads), 0, s, a);
   }
