@@ -31,8 +31,9 @@
  *     fastest).  Outputs must not overlap inputs or each other;
  *   - calls are asynchronous on the handle's stream (ps_soft_set_stream) and read nothing
  *     back: n, entries, k are the host's, ids and row pointers are checked by the kernels.  An
- *     item id >= items, or a row pointer that decreases or lies outside [0, entries], makes that
- *     row's loss NaN (ps_soft_top: is no exclusion); nothing outside the arrays is touched;
+ *     item id >= items makes its row's loss NaN and counts as no target (ps_soft_top: excludes
+ *     nothing); so does a row pointer that decreases or lies outside [0, entries] (its row has no
+ *     list then; where rows' lists overlap, dW is unspecified); nothing outside the arrays is touched;
  *   - the handle owns a workspace that grows to the largest call seen (growing synchronizes the
  *     stream).  A call that is being captured into a graph cannot grow it: run the same call
  *     once before, or ps_soft_reserve; else PS_SOFT_ESTATE.  A handle that has been captured

@@ -1005,14 +1005,15 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     }
   }
   if (a.dX && lane < G) {
-    const float gw = a.t.gw[i], mean = ldexpf(a.t.total[i] / den, -a.scal->ew);
+    const float gw = a.t.gw[i], mean = a.t.total[i] / den;
+    const int ew = a.scal->ew;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int k0 = v * 4 * G + 4 * g;
       if (k0 >= a.K) continue;
       f32x4 out;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) out[u] = act ? gw * fmaf(mean, o[v][u], -acc[v][u]) : 0.f;
+      for (int u = 0; u < 4; ++u) out[u] = act ? gw * (ldexpf(mean * o[v][u], -ew) - acc[v][u]) : 0.f;
       store4(a.dX + i * a.lddx, k0, a.K, a.vec_out, out);
     }
   }
@@ -2117,8 +2118,8 @@ int32_t padded_chunks(int32_t K) {
 // part of the stream that an XCD's L2 sees is an eighth of it.  No piece shorter than 8 tiles, or than 2 where 8 would
 // leave CUs idle (a tile takes about 1 us, a piece's start and its part of the join about 2).
 int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
-  if (forced > 0) return static_cast<int32_t>(std::min<int64_t>(forced, tiles));
   const int64_t groups = up(own_tiles, kWaves);
+  if (forced > 0) return static_cast<int32_t>(std::max<int64_t>(1, std::min({static_cast<int64_t>(forced), tiles, (static_cast<int64_t>(1) << 30) / groups})));
   // many own rows: a piece more costs its part of the join (782 workgroups of 100,000 items: 8 pieces 1292 us and 190 of
   // joining, 4 pieces 1274 and 95, 2 pieces 1387 and 48)
   if (groups >= 512) return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(tiles / 8, groups >= 4096 ? 1 : groups >= 2048 ? 2 : 4)));
@@ -2128,9 +2129,11 @@ int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   return static_cast<int32_t>(std::min({want, most, static_cast<int64_t>(256)}));
 }
 
+constexpr int64_t kFewRows = 4096;
 int64_t few_rows(int64_t n) { return n >= 8 ? 8 : n >= 3 ? 4 : 1; }  // that share a read of W
 
-Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
+// room: enough for calls of fewer rows too, whose pieces may be more (ps_soft_reserve)
+Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw, bool room = false) {
   Plan p{};
   p.np = h->type == PS_SOFT_F32 ? 2 : 1;
   p.k16 = padded_chunks(h->K);
@@ -2148,7 +2151,7 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   p.rsplits = static_cast<int32_t>(up(p.wt, p.rper));
   // in us: packing and the pass take about 12 and the packing's bytes.  One user, 17,770 items, K = 128: 32 -> 24
   const double scores = static_cast<double>(n) * static_cast<double>(h->items);
-  p.few = !dx && !dw && h->splits == 0 && scores * (5 + 0.065 * h->K) * 1e-6 < 12 + h->items * 4e-6 * h->K;
+  p.few = !dx && !dw && h->splits == 0 && n <= kFewRows && scores * (5 + 0.065 * h->K) * 1e-6 < 12 + h->items * 4e-6 * h->K;
   if (p.few) {
     const int64_t rows = up(std::max<int64_t>(n, 1), few_rows(n)), most = up(h->items, kTopGroup);
     p.few_items = up(h->items, std::min<int64_t>(most, up(1024, rows)));
@@ -2183,7 +2186,14 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw) {
   p.scal = a.take(sizeof(Scal));
   p.px = a.take(p.few ? 0 : p.xt * p.x_stride * 2);
   p.pw = a.take(p.few ? 0 : p.wt * p.w_stride * 2);
-  const int64_t rpad = p.rsplits * p.xt * kTile, cpad = p.csplits * p.wt * kTile;
+  int64_t rpad = p.rsplits * p.xt * kTile, cpad = p.csplits * p.wt * kTile;
+  if (room) {
+    // g workgroups of own tiles take at most max(768 / g + 8, 256 / g + 1, 4) pieces (pieces(), or the forced number), and
+    // one row in a piece of k_few's at most 1024 + 32 blocks' pieces of 32 padded rows
+    const int64_t gx = up(p.xt, kWaves), gw = up(p.wt, kWaves), force = h->splits;
+    rpad = std::max<int64_t>(kWaves * kTile * (force > 0 ? force * gx : 768 + 9 * gx), 1056 * kTile + 2 * kFewRows);
+    cpad = kWaves * kTile * (force > 0 ? force * gw : 768 + 9 * gw);
+  }
   p.m = a.take(std::max(rpad, cpad) * 4);
   p.l = a.take(rpad * 4);
   p.o = a.take(std::max(dx ? rpad : 0, cpad) * p.kd * 32 * 4);
@@ -2411,13 +2421,13 @@ bool top_by_candidates(int64_t n, int64_t items, int32_t K) {
   return all > candidates;
 }
 
-TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude) {
+TopPlan top_plan(const ps_soft_t *h, int64_t n, int32_t k, bool exclude, int32_t search) {
   TopPlan p{};
   const int64_t all = std::max<int64_t>(n, 1);
   p.words = static_cast<int32_t>(up(h->items, 32));
   // a threshold needs more groups of 16 items than k: 64 k items leave about k / 8 candidates more than k
   p.filter = h->items >= 64LL * k && top_by_candidates(all, h->items, h->K);
-  if (h->search >= 0) p.filter = h->search == 1;
+  if (search >= 0) p.filter = search == 1;
   p.filter = p.filter && h->items < 1 << 30;  // counts of candidates
   Arena a;
   if (p.filter) {
@@ -2474,7 +2484,7 @@ void run_score(const ScoreArgs &a, int32_t kc, hipStream_t s) {
 template <class T>
 int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64_t ldw, int32_t k, const int64_t *row_ptr,
              const int32_t *item, int64_t entries, int32_t *top_item, float *top_score, int64_t ldo) {
-  const TopPlan p = top_plan(h, n, k, row_ptr != nullptr);
+  const TopPlan p = top_plan(h, n, k, row_ptr != nullptr, h->search);
   const int rc = grow(h, p.bytes);
   if (rc) return rc;
   char *const base = h->work;
@@ -2658,8 +2668,19 @@ int ps_soft_reserve(ps_soft_t *h, int64_t n, int64_t entries, int32_t top) {
   DeviceGuard guard;
   const int rc = open(h, guard);
   if (rc) return rc;
-  int64_t bytes = plan(h, n, entries, true, true).bytes;
-  if (top > 0) bytes = std::max(bytes, top_plan(h, n, top, true).bytes);
+  int64_t bytes = plan(h, n, entries, true, true, true).bytes;
+  if (top > 0) {
+    // what either form takes; the first's rows end where the second is faster, unless `top` rules that out
+    int64_t all = n;
+    if (h->search < 0 && h->items >= 64LL * top && top_by_candidates(n, h->items, h->K)) {
+      int64_t lo = 0;
+      while (lo < all) {
+        const int64_t mid = (lo + all) / 2;
+        if (top_by_candidates(mid, h->items, h->K)) all = mid; else lo = mid + 1;
+      }
+    }
+    bytes = std::max({bytes, top_plan(h, all, top, true, 0).bytes, top_plan(h, n, top, true, 1).bytes});
+  }
   return grow(h, bytes);
 }
 

@@ -411,7 +411,7 @@ def test_numbers_of_far_magnitudes(soft):
     with soft.PsSoft(M, K) as h:
         say("magnitudes: powers of two")
         base = h.xent(X, W, item)
-        for e in (-60, 40, 90):
+        for e in (-100, -60, 40, 90, 100):
             far = h.xent(X * 2.0 ** e, W * 2.0 ** -e, item)
             assert torch.equal(far[0], base[0]) and torch.equal(far[1], base[1])
             assert torch.equal(far[2] * 2.0 ** e, base[2]) and torch.equal(far[3] * 2.0 ** -e, base[3])
@@ -614,6 +614,49 @@ def test_captured_and_replayed(soft):
             big = some(700, 300, 36, 18)
             run_all(h, big)  # the handle grows; the graph's workspace stays
             torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("M,K,dtype", [(300, 36, F32), (20_000, 64, F32), (5000, 256, BF16)])
+def test_reserved_room_holds_every_smaller_call(soft, M, K, dtype):
+    # captured calls cannot grow the workspace: each of these fits what was reserved for the largest
+    with soft.PsSoft(M, K, dtype) as h:
+        h.reserve(3000, 30_000, 50)
+        for n in (1, 2, 5, 17, 40, 100, 130, 257, 513, 800, 1025, 1500, 2049, 3000):
+            g = gen(25, n)
+            X, W = tables(n, M, K, dtype, g)
+            ptr, item = lists(n, M, 30_000 // (4 * n + 8), g, bad=False)
+            ids = torch.randint(0, M, (n, 10), generator=g, dtype=torch.int32).cuda()
+            score = torch.randn(n, 10, generator=g).cuda()
+            say(f"reserved M={M} K={K} n={n} entries={item.numel()}")
+            assert item.numel() <= 30_000
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                outs = [h.xent(X, W, item, row_ptr=ptr, grad=grad) for grad in (False, "X", "W", True)]
+                outs.append(h.distill(X, W, ids, score))
+                outs.append(h.top(X, W, min(50, M), row_ptr=ptr, item=item))
+                outs.append(h.top(X, W, 3))
+            graph.replay()
+            torch.cuda.synchronize()
+            with soft.PsSoft(M, K, dtype) as eager:
+                assert same(outs[3], eager.xent(X, W, item, row_ptr=ptr))
+                assert same(outs[0], eager.xent(X, W, item, row_ptr=ptr, grad=False))
+                assert same(outs[5], eager.top(X, W, min(50, M), row_ptr=ptr, item=item))
+            del graph
+
+
+def test_many_rows_of_few_items(soft):
+    # more rows than a launch has in its second dimension, one item
+    n, K = 70_001, 3
+    X, W = torch.randn(n, K, device="cuda"), torch.randn(1, K, device="cuda")
+    item = torch.zeros(n, dtype=torch.int32, device="cuda")
+    with soft.PsSoft(1, K) as h:
+        loss, lse = h.xent(X, W, item, grad=False)
+        assert torch.allclose(lse, X @ W[0], atol=1e-5) and float(loss.abs().max()) < 1e-5
+        best, score = h.top(X, W, 2)
+        assert (best == torch.tensor([0, -1], device="cuda", dtype=torch.int32)).all()
+        loss, lse, dX, dW = h.xent(X, W, item)
+        assert float(dX.abs().max()) < 1e-5 and float(dW.abs().max()) < 1e-2
 
 
 def test_from_teacher_to_student(soft):
