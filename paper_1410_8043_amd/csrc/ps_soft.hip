@@ -15,7 +15,7 @@
 // so that its largest number lies in [2^13, 2^14) and is held as one plane of fp16 (bf16 and
 // f16 tables: exact for all numbers above 2^-28 of the largest) or as two, h = fp16(x), l =
 // fp16(x - h) (f32 tables: 22 bits, to 2^-38 of the largest below that), and products drop l*l
-// (2^-22).  The weights p' are held in two planes too, except in the pass over the rows of 16-bit tables.  Sums over items and rows, running
+// (2^-22).  The weights p' are held in two planes too, except in the pass over the rows of bf16 tables.  Sums over items and rows, running
 // maxima and log-sum-exps are fp32.
 #include <hip/hip_runtime.h>
 
@@ -520,17 +520,17 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // through LDS, shared by the workgroup, loaded one step ahead of their use.
 // Score instruction: stream rows x own rows, so a lane holds one own row (l%32) and 16 stream rows
 // 8(r/4) + 4h + r%4 of each tile.
+// one_plane (items of bf16 tables): there the weights are the differences (a p - the targets') themselves, so one plane rounds
+// each by at most 2^-11 of itself, an eighth of what the gradient's own rounding does, and a third of the pass's instructions
+// goes (8192 rows x 100,000 items K = 256 1386 -> 1267 us).  Rows' weights are p alone, and the targets come off
+// later: one plane would leave 2^-11 of p where p nearly equals the target, so they have two; so has fp16, whose
+// gradients hold 11 bits themselves.
 // The matrix instructions bound it (1.1 PFLOP/s of them at K = 128 fp32, the clock near 1.85 GHz), so the loop keeps them
 // fed: the next tile's scores are made beside the exponentials of this one's, the sums beside the rounding.
-template <int NP, int KC, int DB, bool COL>
+template <int NP, int KC, int DB, bool COL, bool one_plane>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
   constexpr int KD = KC / 2;
-  // Items of 16-bit tables: the weights are the differences (a p - the targets') themselves, so one plane rounds each by
-  // 2^-12 of itself, an eighth of what the gradient's own rounding to bf16 does (fp16: as much), and a third of the
-  // pass's instructions goes.  Rows' weights are p alone, and the targets come off later: one plane would leave
-  // 2^-12 of p where p nearly equals the target, so they have two.
-  constexpr bool one_plane = COL && NP == 1;
   extern __shared__ _Float16 buf[];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -899,8 +899,9 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   const float mine = top;
   top = wave_max(top);
   den = wave_sum(den * __builtin_amdgcn_exp2f(mine - top));
-  const float lse2 = top - kShift + log2f(den);
-  const float lse = lse2 * 0.69314718055994530942f;
+  // in 64 bits: the loss is what is left of total lse - x . c, and lse2 in 32 would be off by 5e-7 at 8 .. 16
+  const double lse64 = static_cast<double>(top - kShift) + log2(static_cast<double>(den)), lse = lse64 * 0.69314718055994530942;
+  const float lse2 = static_cast<float>(lse64);
   f32x4 acc[V], o[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -985,20 +986,21 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
       }
     }
   }
-  float d = 0.f;  // x . c
+  double d = 0.0;  // x . c
   if (act) {
     f32x4 x[V];
     load_row<T, G, V>(x, a.x.p + i * a.x.ld, g, a.K, a.x.vec);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) d = fmaf(x[v][u], acc[v][u], d);
+      for (int u = 0; u < 4; ++u) d = fma(static_cast<double>(x[v][u]), static_cast<double>(acc[v][u]), d);
 #pragma unroll
     for (int s = G / 2; s > 0; s >>= 1) d += __shfl_xor(d, s);
   }
   if (lane == 0) {
-    if (a.loss) a.loss[i] = act || a.t.extra[i] != 0.f ? a.t.tau * a.t.tau * (a.t.extra[i] + fmaf(a.t.total[i], lse, -d / a.t.tau)) : 0.f;
-    if (a.lse) a.lse[i] = lse;
+    if (a.loss)
+      a.loss[i] = act || a.t.extra[i] != 0.f ? static_cast<float>(a.t.tau * a.t.tau * (a.t.extra[i] + (a.t.total[i] * lse - d / a.t.tau))) : 0.f;
+    if (a.lse) a.lse[i] = static_cast<float>(lse);
     if (a.rowvec) {
       a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 : -__builtin_inff();
       a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.t.share[i] / a.scal->amax : 0.f;
@@ -2205,37 +2207,42 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw, bool
   return p;
 }
 
+void hip_launch(void (*f)(PassArgs), dim3 grid, unsigned lds, const PassArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL(f, grid, dim3(64 * kWaves), lds, s, a);
+}
+
 template <int NP, int KC, int DB>
-void launch_pass(const PassArgs &a, bool col, hipStream_t s) {
+void launch_pass(const PassArgs &a, bool col, bool one_plane, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(up(a.own_tiles, kWaves) * a.splits));
   const unsigned lds = static_cast<unsigned>(stage_of(NP, KC, DB, col).halves * 2);
-  if (col) {
-    if constexpr (DB > 0) hipLaunchKernelGGL((k_pass<NP, KC, DB, true>), grid, dim3(64 * kWaves), lds, s, a);
-  } else {
-    hipLaunchKernelGGL((k_pass<NP, KC, DB, false>), grid, dim3(64 * kWaves), lds, s, a);
+  if (!col) {
+    hip_launch((k_pass<NP, KC, DB, false, false>), grid, lds, a, s);
+  } else if constexpr (DB > 0) {
+    if constexpr (NP == 1) {
+      if (one_plane) return hip_launch((k_pass<NP, KC, DB, true, true>), grid, lds, a, s);
+    }
+    hip_launch((k_pass<NP, KC, DB, true, false>), grid, lds, a, s);
   }
 }
 
-// sums: the pass also sums rows.  512 numbers of two planes leave no registers for all sums: two launches of half of
-// them each, with the scores made twice.
 template <int NP, int KC>
-void run_pass_of(PassArgs a, bool col, bool sums, hipStream_t s) {
+void run_pass_of(PassArgs a, bool col, bool sums, bool one_plane, hipStream_t s) {
   constexpr int KD = KC / 2, DB = std::min(KD, 8);
   a.d0 = 0;
-  if (!sums) launch_pass<NP, KC, 0>(a, false, s);
+  if (!sums) launch_pass<NP, KC, 0>(a, false, false, s);
   else
-    for (; a.d0 < KD; a.d0 += DB) launch_pass<NP, KC, DB>(a, col, s);
+    for (; a.d0 < KD; a.d0 += DB) launch_pass<NP, KC, DB>(a, col, one_plane, s);
 }
 template <int NP>
-void run_pass(const PassArgs &a, int k16, bool col, bool sums, hipStream_t s) {
+void run_pass(const PassArgs &a, int k16, bool col, bool sums, bool one_plane, hipStream_t s) {
   switch (k16) {
-    case 2: return run_pass_of<NP, 2>(a, col, sums, s);
-    case 4: return run_pass_of<NP, 4>(a, col, sums, s);
-    case 6: return run_pass_of<NP, 6>(a, col, sums, s);
-    case 8: return run_pass_of<NP, 8>(a, col, sums, s);
-    case 12: return run_pass_of<NP, 12>(a, col, sums, s);
-    case 16: return run_pass_of<NP, 16>(a, col, sums, s);
-    default: return run_pass_of<NP, 32>(a, col, sums, s);
+    case 2: return run_pass_of<NP, 2>(a, col, sums, one_plane, s);
+    case 4: return run_pass_of<NP, 4>(a, col, sums, one_plane, s);
+    case 6: return run_pass_of<NP, 6>(a, col, sums, one_plane, s);
+    case 8: return run_pass_of<NP, 8>(a, col, sums, one_plane, s);
+    case 12: return run_pass_of<NP, 12>(a, col, sums, one_plane, s);
+    case 16: return run_pass_of<NP, 16>(a, col, sums, one_plane, s);
+    default: return run_pass_of<NP, 32>(a, col, sums, one_plane, s);
   }
 }
 
@@ -2319,7 +2326,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       a.scal = scal;
       a.scale = scale;
       a.tiles_per_split = p.rper;
-      run_pass<NP>(a, p.k16, false, dx, s);
+      run_pass<NP>(a, p.k16, false, dx, false, s);
     }
     RowArgs<T> r{};
     r.t = t;
@@ -2372,7 +2379,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       a.tiles_per_split = p.cper;
       a.first = t.entries > 0 ? first : nullptr;
       a.pay = rec[from].pay;
-      run_pass<NP>(a, p.k16, true, true, s);
+      run_pass<NP>(a, p.k16, true, true, std::is_same<T, bf16_t>::value, s);
     }
   }
   if (dw) {

@@ -6,7 +6,7 @@ Bounds, per value, u = 2^-24 half a step of fp32:
     22 bits (three products dropped or rounded at 2^-22 each make 12 u), and the scaling;
   * a weight exp(s - lse) is off by that of s and of lse, and 2^-20 of the exponential and of its two
     planes of 22 bits; a sum of M of them adds (M + 64) u;
-  * tables of 16 bits: the item gradients' weights g (V p - y) are held in one fp16 number each, off by half a step,
+  * bf16 tables: the item gradients' weights g (V p - y) are held in one fp16 number each, off by half a step,
     2^-11 of themselves (2^-25 of the largest share below 2^-14 of it, within the 2^-34 of the shares' sums below);
   * what is rounded to the tables' type adds half a step of it, and half its smallest step.
 """
@@ -83,7 +83,7 @@ def xent(X, W, item, row_ptr=None, value=None, weight=None):
     live = np.zeros(n, bool)
     live[rows] = True
     wt = np.ones(n) if weight is None else f64(weight)
-    return dense_loss(x, w, y, np.zeros(n), live, wt, 1.0, X.dtype != torch.float32)
+    return dense_loss(x, w, y, np.zeros(n), live, wt, 1.0, X.dtype == torch.bfloat16)
 
 
 def distill(X, W, item, score, tau, tlse=None, weight=None):
@@ -108,7 +108,7 @@ def distill(X, W, item, score, tau, tlse=None, weight=None):
     r, c = np.nonzero(here)
     np.add.at(y, (r, it[r, c]), q[r, c])
     wt = np.ones(n) if weight is None else f64(weight)
-    vals, errs = dense_loss(x, w, y, extra, live, wt, tau, X.dtype != torch.float32)
+    vals, errs = dense_loss(x, w, y, extra, live, wt, tau, X.dtype == torch.bfloat16)
     # q itself comes from fp32: each is off by eq of itself, t and z up to 4 u of themselves
     live = live & (wt != 0)
     eq = 2.0 ** -20 + 8 * U * (np.abs(np.where(here, t, 0.0)).max(1) + np.abs(np.where(live, z[:, 0], 0.0)))
