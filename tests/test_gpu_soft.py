@@ -4,6 +4,8 @@ Sizes from one row and one item to several tiles and pieces, odd ones among them
 and misaligned tables; lists that are empty, repeat, are padded or out of range; masked rows that hold NaN;
 other streams, captured graphs, two handles; equal bits of equal calls.
 """
+import contextlib
+import gc
 import sys
 
 import numpy as np
@@ -30,6 +32,19 @@ def soft():
 def say(msg):
     print(msg, flush=True)
     sys.stdout.flush()
+
+
+@contextlib.contextmanager
+def capture(graph):
+    """torch.cuda.graph without the garbage collector: a graph left in a cycle (an exception's frames hold
+    one) that it frees inside a capture waits for the device there, which ends the process."""
+    gc.collect()
+    gc.disable()
+    try:
+        with torch.cuda.graph(graph):
+            yield
+    finally:
+        gc.enable()
 
 
 def gen(*seed):
@@ -586,10 +601,10 @@ def test_captured_and_replayed(soft):
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with pytest.raises(soft.PsSoftError) as err:
-            with torch.cuda.graph(graph):
+            with capture(graph):
                 fresh.xent(d["X"], d["W"], d["item"], row_ptr=d["ptr"])
         assert err.value.code == soft.ESTATE
-        del graph
+        del graph, err
         torch.cuda.synchronize()
     with soft.PsSoft(300, 36) as h, soft.PsSoft(300, 36) as eager:
         n_entries = max(x["item"].numel() for x in (d, e))
@@ -597,7 +612,7 @@ def test_captured_and_replayed(soft):
         static = {k: v.clone() for k, v in d.items()}
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
+        with capture(graph):
             out = run_all(h, static)
         for k in range(4):
             src = (d, e)[k % 2]
@@ -631,7 +646,7 @@ def test_reserved_room_holds_every_smaller_call(soft, M, K, dtype):
             assert item.numel() <= 30_000
             torch.cuda.synchronize()
             graph = torch.cuda.CUDAGraph()
-            with torch.cuda.graph(graph):
+            with capture(graph):
                 outs = [h.xent(X, W, item, row_ptr=ptr, grad=grad) for grad in (False, "X", "W", True)]
                 outs.append(h.distill(X, W, ids, score))
                 outs.append(h.top(X, W, min(50, M), row_ptr=ptr, item=item))
