@@ -50,6 +50,10 @@ constexpr float kNone = -1e30f; // reference before the first tile: finite, so t
 // kLag: p' stays below 2^15, and a weight of 2^-17 of the largest keeps 22 bits
 constexpr float kShift = 7.f, kLag = 8.f;
 
+// A launch holds less than 2^32 threads in a dimension: workgroups beyond 2^22 go to the second
+constexpr int kGridBits = 22;
+__device__ inline int32_t block_index() { return static_cast<int32_t>(blockIdx.y << kGridBits | blockIdx.x); }
+
 // ------------------------------------------------------------------ element types
 struct bf16_t { uint16_t u; };
 struct f16_t { _Float16 h; };
@@ -326,10 +330,12 @@ __global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackS
                                                    Scal *scal) {
   extern __shared__ float tile[];  // [32][32 min(kd, kPackBlocks) + 1]
   __shared__ float sh[4];
-  const bool second = static_cast<int32_t>(blockIdx.x) >= px.tiles;
+  const int32_t block = block_index();
+  const bool second = block >= px.tiles;
   const Table<T> t = second ? w : x;
   const PackSide ps = second ? pw : px;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) - (second ? px.tiles : 0);
+  const int64_t at = static_cast<int64_t>(block) - (second ? px.tiles : 0);
+  if (at >= ps.tiles) return;
   const float most = block_max(part[(second ? kParts : 0) + threadIdx.x], sh);
   const int ex = scale_exp(most);
   if (at == 0) {
@@ -466,15 +472,16 @@ __host__ __device__ constexpr Stage stage_of(int np, int kc, int db, bool col) {
 // The sorted target records of one own tile, in windows of 64, one per lane, two windows read ahead
 struct Window {
   const uint2 *pay;
-  int at, end, pos;
+  uint32_t at, end;  // up to 2^31, and reads 128 ahead
+  int pos;
   uint32_t due;  // the next record's row
   uint2 now, next[2];
   // a record behind the last: a row above all
-  __device__ uint2 get(int i) const { return i < end ? pay[i] : make_uint2(0xffffffffu, 0u); }
+  __device__ uint2 get(uint32_t i) const { return i < end ? pay[i] : make_uint2(0xffffffffu, 0u); }
   __device__ void open(const uint2 *p, int64_t b, int64_t e, int lane) {
     pay = p + b;
     at = lane;
-    end = static_cast<int>(e - b);
+    end = static_cast<uint32_t>(e - b);
     pos = 0;
     now = get(at);
     next[0] = get(at + 64);
@@ -534,8 +541,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   extern __shared__ _Float16 buf[];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x % a.splits;
-  const int64_t own_tile = static_cast<int64_t>(blockIdx.x / a.splits) * kWaves + wave;
+  const int32_t block = block_index();
+  const int split = block % a.splits;
+  const int64_t own_tile = static_cast<int64_t>(block / a.splits) * kWaves + wave;
+  if (own_tile - wave >= a.own_tiles) return;
   const int64_t tiles = (a.str_rows + kTile - 1) / kTile;
   const int t0 = static_cast<int>(split * a.tiles_per_split);
   const int t1 = static_cast<int>(min(t0 + a.tiles_per_split, tiles));
@@ -878,7 +887,7 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = lane & (G - 1);
   const int grp = (TW > 1 ? wave * (64 / G) : 0) + lane / G;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * RB + (TW == 1 ? wave : 0);
+  const int64_t i = static_cast<int64_t>(block_index()) * RB + (TW == 1 ? wave : 0);
   const int64_t row_end = (a.t.n + kTile - 1) / kTile * kTile;
   if (i >= a.t.n) {  // rows behind the last, to the end of its tile: no weight in the pass over rows
     if (a.rowvec && i < row_end && lane == 0 && (TW == 1 || wave == 0)) {
@@ -1320,7 +1329,7 @@ struct ItemArgs {
 template <class T, int G, int V>
 __global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
   const int g = threadIdx.x & (G - 1);
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * (kThreads / G) + threadIdx.x / G;
+  const int64_t j = static_cast<int64_t>(block_index()) * (kThreads / G) + threadIdx.x / G;
   if (j >= a.items) return;
   const float back = a.splits ? ldexpf(a.scal->amax, -a.scal->ex) : 0.f;
   f32x4 o[V];
@@ -1669,9 +1678,11 @@ __global__ __launch_bounds__(kThreads) void k_top_pack(Table<T> x, Table<T> w, i
                                                        int32_t K, int32_t kc, float c, const float *part, int32_t *count) {
   extern __shared__ float tile[];
   __shared__ float sh[4], norm[kTile];
-  const bool second = static_cast<int32_t>(blockIdx.x) >= xt;
+  const int32_t block = block_index();
+  const bool second = block >= xt;
   const Table<T> t = second ? w : x;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) - (second ? xt : 0);
+  const int64_t at = static_cast<int64_t>(block) - (second ? xt : 0);
+  if (second && at * kTile >= w.rows) return;
   int ex = 0;
   if constexpr (!std::is_same<T, f16_t>::value) ex = scale_exp(block_max(part[(second ? kParts : 0) + threadIdx.x], sh));
   const int64_t begin = second ? 0 : row0, end = second ? t.rows : row0 + rows;
@@ -2082,6 +2093,11 @@ unsigned blocks_for(int64_t n, int64_t per, int64_t most) {
   return static_cast<unsigned>(std::max<int64_t>(1, std::min(up(n, per), most)));
 }
 
+dim3 grid_of(int64_t blocks) {  // for kernels that use block_index(); the last dimension's surplus returns at once
+  const int64_t most = 1LL << kGridBits;
+  return dim3(static_cast<unsigned>(std::min(blocks, most)), static_cast<unsigned>(up(blocks, most)));
+}
+
 int32_t row_lanes(int32_t K) {  // lanes of 4 numbers for a row, a power of two
   int32_t n = 1;
   while (4 * n < K) n *= 2;
@@ -2213,7 +2229,7 @@ void hip_launch(void (*f)(PassArgs), dim3 grid, unsigned lds, const PassArgs &a,
 
 template <int NP, int KC, int DB>
 void launch_pass(const PassArgs &a, bool col, bool one_plane, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(up(a.own_tiles, kWaves) * a.splits));
+  const dim3 grid = grid_of(up(a.own_tiles, kWaves) * a.splits);
   const unsigned lds = static_cast<unsigned>(stage_of(NP, KC, DB, col).halves * 2);
   if (!col) {
     hip_launch((k_pass<NP, KC, DB, false, false>), grid, lds, a, s);
@@ -2252,7 +2268,7 @@ void run_rows(const RowArgs<T> &a, hipStream_t s) {
   // wavefronts per row: all that 256 CUs hold, for lists long enough
   if (a.t.n <= 256) hipLaunchKernelGGL((k_row_finish<T, G, V, 16>), dim3(static_cast<unsigned>(rows)), dim3(1024), 0, s, a);
   else if (a.t.n <= 2048) hipLaunchKernelGGL((k_row_finish<T, G, V, 4>), dim3(static_cast<unsigned>(rows)), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((k_row_finish<T, G, V, 1>), dim3(static_cast<unsigned>(up(rows, 4))), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((k_row_finish<T, G, V, 1>), grid_of(up(rows, 4)), dim3(kThreads), 0, s, a);
 }
 
 // Lanes per row: 4 numbers each, 8 above 256
@@ -2313,7 +2329,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     } else {
       hipLaunchKernelGGL((k_absmax<T>), dim3(2 * kParts), dim3(kScanThreads), 0, s, x, w, h->K, row_lanes(h->K), at_f(p.part));
       const PackSide sx{px, p.x_stride, static_cast<int32_t>(p.xt), dw}, sw{pw, p.w_stride, static_cast<int32_t>(p.wt), dx};
-      hipLaunchKernelGGL((k_pack<T, NP>), dim3(static_cast<unsigned>(p.xt + p.wt)), dim3(kThreads),
+      hipLaunchKernelGGL((k_pack<T, NP>), grid_of(p.xt + p.wt), dim3(kThreads),
                          static_cast<unsigned>(kTile * (std::min(p.kd, kPackBlocks) * 32 + 1) * 4), s, x, w, sx, sw, h->K, p.k16, p.kd, at_f(p.part),
                          at_f(p.row_part), static_cast<int32_t>(row_blocks), scal);
       a.own = px;
@@ -2396,7 +2412,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     a.lddw = lddw;
     a.vec_out = aligned4(dW, lddw);
     by_k(h->K, [&](auto g, auto v) {
-      hipLaunchKernelGGL((k_item_finish<T, g(), v()>), dim3(static_cast<unsigned>(up(h->items, kThreads / g()))), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL((k_item_finish<T, g(), v()>), grid_of(up(h->items, kThreads / g())), dim3(kThreads), 0, s, a);
     });
   }
   SOFT_TRY(h, hipGetLastError());
@@ -2544,7 +2560,7 @@ int soft_top(ps_soft_t *h, int64_t n, const T *X, int64_t ldx, const T *W, int64
     const int64_t xt = up(a.n, kTile);
     const float c = (h->type == PS_SOFT_F32 ? 0x1p-10f + 0x1p-22f : 0.f) + (2 * p.kc + 16) * 0x1p-22f + std::sqrt(static_cast<float>(h->K)) * 0x1p-24f;
     const int kd = std::min((h->K + 31) / 32, kPackBlocks);
-    hipLaunchKernelGGL((k_top_pack<T>), dim3(static_cast<unsigned>(xt + (a.row0 ? 0 : p.wt))), dim3(kThreads),
+    hipLaunchKernelGGL((k_top_pack<T>), grid_of(xt + (a.row0 ? 0 : p.wt)), dim3(kThreads),
                        static_cast<unsigned>(kTile * (kd * 32 + 1) * 4), s, a.x, a.w, a.row0, a.n, static_cast<int32_t>(xt), px, pw, h->K,
                        p.kc, c, part, count);
     q.own = px;

@@ -697,3 +697,40 @@ def test_from_teacher_to_student(soft):
             got = student.distill(X, W, item, score, tau=2.0)
             check(f"step {step}", got, vals, bounds, F32)
             X, W = X - 0.05 * got[2], W - 0.05 * got[3]
+
+
+@pytest.mark.parametrize("n,M,K", [(2**24 + 5, 2, 1), (3, 2**24 + 5, 129)])
+def test_more_workgroups_than_a_launch_dimension_takes(soft, n, M, K):
+    # 2^22 workgroups of 4 rows, or of 4 items, and a few more rows; three kinds of rows, five of items
+    xs, ws = torch.arange(n, device="cuda") % 3, torch.arange(M, device="cuda") % 5
+    X = torch.zeros(n, K, dtype=BF16, device="cuda")
+    W = torch.zeros(M, K, dtype=BF16, device="cuda")
+    X[:, 0], W[:, 0] = (xs - 1) / 8, ws - 2
+    item = (torch.arange(n, device="cuda") * 7919 % M).int()
+    item[-1] = M - 1
+    at = item.long()
+    weight = float(2**24) if M > n else 1.0  # gradients of about 1
+    with soft.PsSoft(M, K, BF16) as h:
+        loss, lse, dX, dW = h.xent(X, W, item, weight=torch.full((n,), weight, device="cuda"))
+    # by kinds, in 64 bits: M/5 items each, n/3 rows each
+    nw, nx = torch.bincount(ws, minlength=5).double(), torch.bincount(xs, minlength=3).double()
+    w, x = torch.arange(-2.0, 3, device="cuda").double(), torch.arange(-1.0, 2, device="cuda").double() / 8
+    e = (x[:, None] * w).exp()
+    total = (e * nw).sum(1)
+    # values up to 2^5 rounded to half of 2^-19, and weights to 2^-21 (the exponent's and their own rounding)
+    near = 2**-20 + 2**-20
+    want = total.log()[xs]
+    assert float((lse - want).abs().max()) <= near
+    assert float((loss - (want - x[xs] * w[ws[at]])).abs().max()) <= near
+    # dX: bf16's half step; sums of numbers up to 2 in pieces of 2 x 2048 instructions, half a step of fp32 each
+    gx = weight * (((e * nw * w).sum(1) / total)[xs] - w[ws[at]])
+    assert float(((dX[:, 0] - gx).abs() - 2**-8 * gx.abs()).max()) <= weight * 2**-11
+    # dW: the same, weights of one plane of fp16, and, in a tile of 32 items with targets, to 2^-25 of 2 weight
+    p = weight * e / total[:, None] * nx[:, None]
+    gw = (p * x[:, None]).sum(0)[ws].index_add_(0, at, -weight * x[xs])
+    size = (p * x.abs()[:, None]).sum(0)[ws].index_add_(0, at, weight * x[xs].abs())
+    tile = torch.zeros(M // 32 + 1, dtype=torch.float64, device="cuda").index_fill_(0, at // 32, weight * n * 2**-24)
+    slack = 2**-8 * gw.abs() + 2**-10 * size + tile[torch.arange(M, device="cuda") // 32]
+    assert float(((dW[:, 0] - gw).abs() - slack).max()) <= 0
+    if K > 1:
+        assert not dX[:, 1:].any() and not dW[:, 1:].any()
