@@ -168,7 +168,8 @@ __global__ __launch_bounds__(kThreads) void k_fill_keys(int32_t *key, int64_t en
     key[e] = dead;
 }
 
-// One wavefront per row.  Bound by the reads of the lists and the writes of the records.
+// One wavefront per row.  Bound by the reads of the lists and the writes of the records (16,384 rows, 3.4M entries: 27 us,
+// 2.5 TB/s).
 template <bool Distill>
 __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
   __shared__ float sh[4];
@@ -265,7 +266,8 @@ struct Table {
 };
 
 // Largest finite magnitude of each table, kParts partial maxima each.  A row's numbers by as many lanes as its float4s,
-// rounded up to a power of two; bound by memory (51 MB at 4.4 TB/s; with a division per float4 it was 0.9).
+// rounded up to a power of two; bound by memory and by latency (55 MB in 20 us, 2.7 TB/s; with a
+// division per float4 it was 0.9).
 constexpr int kScanThreads = 1024;
 template <class T>
 __global__ __launch_bounds__(kScanThreads) void k_absmax(Table<T> x, Table<T> w, int32_t K, int32_t lanes, float *part) {
@@ -323,7 +325,8 @@ struct PackSide {
 // 16c + 8(l/32) ..+7; and turned, for the sums, rows 16q ..+15 and numbers 32b ..+31: lane l holds
 // number 32b + l%32 of the rows that the score instruction leaves in this lane's registers
 // 8q .. 8q+7, 16q + {4h ..+3, 8 + 4h ..+3} with h = l/32: so weights go from one matrix instruction to
-// the next without a move.  One workgroup per tile; bound by memory.
+// the next without a move.  One workgroup per tile; bound by memory (8192 + 100,000 rows, K = 256 bf16: 165 MB in 31 us,
+// 5.3 TB/s).
 template <class T, int NP>
 __global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackSide px, PackSide pw, int32_t K, int32_t k16,
                                                    int32_t kd, const float *part, const float *row_part, int32_t row_parts,
@@ -532,8 +535,12 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // goes (8192 rows x 100,000 items K = 256 1386 -> 1267 us).  Rows' weights are p alone, and the targets come off
 // later: one plane would leave 2^-11 of p where p nearly equals the target, so they have two; so has fp16, whose
 // gradients hold 11 bits themselves.
-// The matrix instructions bound it (1.1 PFLOP/s of them at K = 128 fp32, the clock near 1.85 GHz), so the loop keeps them
-// fed: the next tile's scores are made beside the exponentials of this one's, the sums beside the rounding.
+// The matrix instructions bound rows over items (1.16 PFLOP/s of them at K = 128 fp32, 1.14 at K = 256 bf16; a large
+// library product reaches 1.2), so the loop keeps them fed: the next tile's scores are made beside the exponentials of this one's,
+// the sums beside the rounding.  Items over rows have the records and the shares besides (K = 128 fp32 385 / 510 us), and
+// with one plane fewer matrix instructions to hide 85 others a tile behind (K = 128 bf16 0.67 PFLOP/s).  The tiles' way
+// from L2 is a seventh to a fifth of it: 8 wavefronts a workgroup, which halve that, 320 / 360 us for 331 / 316; two own tiles a
+// wavefront, which halve the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
 template <int NP, int KC, int DB, bool COL, bool one_plane>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
@@ -877,7 +884,8 @@ struct RowArgs {
 };
 
 // TW wavefronts per row (more for few rows).  The targets' part is c_i = sum coef w_j: dX_i needs it, and the loss
-// too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it.
+// too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it
+// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 212 us, 8.2 TB/s, four fifths of it from L2).
 template <class T, int G, int V, int TW>
 __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowArgs<T> a) {
   constexpr int NG = TW * 64 / G;      // groups per row
@@ -1101,7 +1109,7 @@ __device__ inline double dot64(const double *x, const T *w, int l, int K, bool v
 //
 // Log-sum-exps of R rows over pieces of the items: scores in 64 bits from the tables as they are (ps_soft_top's), the sums
 // in fp32 with the maximum of what a lane has seen.  Reads W once for R rows; nothing is packed.  Bound by that
-// read and by latency.
+// read and by latency (one row, 9.1 MB: 4.6 us, 2 TB/s).
 struct FewArgs {
   int64_t n, own_pad;
   int32_t items, K;
@@ -1171,7 +1179,8 @@ static_assert(kShift == 7.f, "k_few's sums");
 // A stable sort of the records by their key, up to 10 bits a pass (one pass up to 32,736 items): records of a tile stay
 // in row order, which the pass over rows relies on, and nothing depends on the order of atomics.  A workgroup
 // takes 4096 records, a wavefront 1024 of them in order; the rank of a record among its wavefront's
-// equal digits comes from the lanes' ballots.  Bound by the scattered writes of the payloads.
+// equal digits comes from the lanes' ballots.  Bound by the scattered writes of the payloads (3.4M records: 47 us, and 19
+// for the counts).
 constexpr int kBins = 1024, kSortTile = 4096, kSortThreads = 512, kSortWaves = kSortThreads / 64;
 
 __global__ __launch_bounds__(kThreads) void k_sort_count(const int32_t *key, int64_t n, int shift, int bins, int32_t *hist, int32_t blocks) {
@@ -1325,7 +1334,7 @@ struct ItemArgs {
   bool vec_out;
 };
 
-// dW_j: the passes' pieces joined.  Bound by memory.
+// dW_j: the passes' pieces joined.  Bound by memory (100,000 items in 4 pieces, K = 256 bf16: 461 MB in 100 us, 4.6 TB/s).
 template <class T, int G, int V>
 __global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
   const int g = threadIdx.x & (G - 1);
@@ -1502,7 +1511,8 @@ __device__ inline void top_out(const TopArgs<T> &a, int64_t r, Best b) {
 // Scores of R rows with groups of 64 items, as keys, and each row's largest key of the group.  A row's k best lie in
 // the groups whose largest key is among the k largest of these (equal ones too), so the second kernel looks at few
 // more than k groups.  A workgroup takes `per` groups, so that many rows load their numbers and lists less often.
-// Bound by the reads of the items' rows, once for R rows, and by latency.
+// Bound by the reads of the items' rows, once for R rows, and by latency for few rows (one, 9.1 MB: 5.5 us), else by the
+// products in 64 bits (64 rows x 20,000 items, K = 64: 20 us).
 constexpr int kTopGroup = 64, kTopGroups = 8;  // items of a group; most groups of a workgroup
 template <class T, int R>
 __global__ __launch_bounds__(kThreads) void k_top_scores(TopArgs<T> a, int per) {
@@ -1754,7 +1764,8 @@ struct ScoreArgs {
   int32_t *found, *count;
 };
 
-// First pass (Find = false) or second.  A wavefront owns 64 rows; the matrix instructions' rate bounds both.
+// First pass (Find = false) or second.  A wavefront owns 64 rows; the matrix instructions' rate bounds both (8192 rows x
+// 17,770 items, K = 128: 46 us, 0.9 PFLOP/s, and 62 with the tests and lists).
 template <int KC, bool Find>
 __global__ __launch_bounds__(kThreads, 2) void k_score(ScoreArgs a) {
   constexpr int kStage = kScoreTiles * KC * kFrag, kRowRoom = row_room(KC);
@@ -1925,7 +1936,8 @@ __device__ inline uint32_t order_bits(float v) {
 }
 __device__ inline float bits_value(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
 
-// T of each row: the k-th largest of its bounds, rounded down.  One workgroup per row; bound by the reads of the bounds.
+// T of each row: the k-th largest of its bounds, rounded down.  One workgroup per row; bound by the reads of the bounds
+// (8192 rows of 1112: 28 us).
 __global__ __launch_bounds__(kThreads) void k_top_least(const float *most, int64_t per_row, int32_t k, float *least) {
   __shared__ int32_t hist[2048], sh[6];
   const float *row = most + blockIdx.x * per_row;
@@ -1933,7 +1945,8 @@ __global__ __launch_bounds__(kThreads) void k_top_least(const float *most, int64
   if (threadIdx.x == 0) least[blockIdx.x] = u ? bits_value(u) : -__builtin_inff();
 }
 
-// The candidates of a row (or all items) in order
+// The candidates of a row (or all items) in order.  Gathers of w rows bound it, and the sort (8192 rows, about 80 candidates:
+// 80 us)
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_top_rank(TopArgs<T> a) {
   __shared__ double x[kMaxK];
@@ -2167,7 +2180,7 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw, bool
   p.rsplits = pieces(p.xt, p.wt, h->splits);
   p.rper = up(p.wt, p.rsplits);
   p.rsplits = static_cast<int32_t>(up(p.wt, p.rper));
-  // in us: packing and the pass take about 12 and the packing's bytes.  One user, 17,770 items, K = 128: 32 -> 24
+  // in us: packing and the pass take about 12 and the packing's bytes.  One user, 17,770 items, K = 128: 32 -> 22
   const double scores = static_cast<double>(n) * static_cast<double>(h->items);
   p.few = !dx && !dw && h->splits == 0 && n <= kFewRows && scores * (5 + 0.065 * h->K) * 1e-6 < 12 + h->items * 4e-6 * h->K;
   if (p.few) {
