@@ -472,35 +472,32 @@ __host__ __device__ constexpr Stage stage_of(int np, int kc, int db, bool col) {
   return s;
 }
 
-// The sorted target records of one own tile, in windows of 64, one per lane, two windows read ahead
+// The sorted target records of one own tile, in windows of 64, one per lane, the next one read ahead
 struct Window {
   const uint2 *pay;
-  uint32_t at, end;  // up to 2^31, and reads 128 ahead
-  int pos;
-  uint32_t due;  // the next record's row
-  uint2 now, next[2];
+  int left, pos;  // records from the lane's on (up to 2^31, so that a place and 64 more would not do)
+  uint32_t due;   // the next record's row
+  uint2 now, next;
   // a record behind the last: a row above all
-  __device__ uint2 get(uint32_t i) const { return i < end ? pay[i] : make_uint2(0xffffffffu, 0u); }
+  __device__ uint2 get(int lane, int ahead) const { return ahead < left ? pay[lane + ahead] : make_uint2(0xffffffffu, 0u); }
   __device__ void open(const uint2 *p, int64_t b, int64_t e, int lane) {
     pay = p + b;
-    at = lane;
-    end = static_cast<uint32_t>(e - b);
+    left = static_cast<int>(e - b) - lane;
     pos = 0;
-    now = get(at);
-    next[0] = get(at + 64);
-    next[1] = get(at + 128);
+    now = get(lane, 0);
+    next = get(lane, 64);
     due = __builtin_amdgcn_readfirstlane(now.x) >> 5;
   }
-  __device__ void step() {
-    at += 64;
+  __device__ void step(int lane) {
+    pay += 64;
+    left -= 64;
     pos = 0;
-    now = next[0];
-    next[0] = next[1];
-    next[1] = get(at + 128);
+    now = next;
+    next = get(lane, 64);
   }
-  __device__ void skip(int n) {  // n records are done
+  __device__ void skip(int n, int lane) {  // n records are done
     pos += n;
-    if (pos == 64) step();
+    if (pos == 64) step(lane);
     due = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(now.x), pos)) >> 5;
   }
 };
@@ -532,7 +529,7 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // 8(r/4) + 4h + r%4 of each tile.
 // one_plane (items of bf16 tables): there the weights are the differences (a p - the targets') themselves, so one plane rounds
 // each by at most 2^-11 of itself, an eighth of what the gradient's own rounding does, and a third of the pass's instructions
-// goes (8192 rows x 100,000 items K = 256 1386 -> 1267 us).  Rows' weights are p alone, and the targets come off
+// goes (8192 rows x 100,000 items K = 256 1386 -> 1267 us, now 1225).  Rows' weights are p alone, and the targets come off
 // later: one plane would leave 2^-11 of p where p nearly equals the target, so they have two; so has fp16, whose
 // gradients hold 11 bits themselves.
 // The matrix instructions bound rows over items (1.16 PFLOP/s of them at K = 128 fp32, 1.14 at K = 256 bf16; a large
@@ -770,7 +767,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
               const uint32_t r = (win.now.x >> 5) & 15, c = win.now.x & 31;
               atomicAdd(y + c * 16 + (((r >> 2) ^ ((c >> 2) & 3)) << 2) + (r & 3), __uint_as_float(win.now.y) * unit);
             }
-            win.skip(n);
+            win.skip(n, lane);
           }
           if (some) {
             __builtin_amdgcn_wave_barrier();
