@@ -882,7 +882,7 @@ struct RowArgs {
 
 // TW wavefronts per row (more for few rows).  The targets' part is c_i = sum coef w_j: dX_i needs it, and the loss
 // too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it
-// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 212 us, 8.2 TB/s, four fifths of it from L2).
+// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 212 us, 8.2 TB/s, 58% of it from L2).
 template <class T, int G, int V, int TW>
 __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowArgs<T> a) {
   constexpr int NG = TW * 64 / G;      // groups per row
