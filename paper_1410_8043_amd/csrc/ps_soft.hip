@@ -15,8 +15,8 @@
 // so that its largest number lies in [2^13, 2^14) and is held as one plane of fp16 (bf16 and
 // f16 tables: exact for all numbers above 2^-28 of the largest) or as two, h = fp16(x), l =
 // fp16(x - h) (f32 tables: 22 bits, to 2^-38 of the largest below that), and products drop l*l
-// (2^-22).  The weights p' are held in two planes too, except in the pass over the rows of bf16 tables.  Sums over items and rows, running
-// maxima and log-sum-exps are fp32.
+// (2^-22).  The weights p' are held in two planes too.  Sums over items and rows, running maxima and log-sum-exps
+// are fp32.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -527,18 +527,14 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // through LDS, shared by the workgroup, loaded one step ahead of their use.
 // Score instruction: stream rows x own rows, so a lane holds one own row (l%32) and 16 stream rows
 // 8(r/4) + 4h + r%4 of each tile.
-// one_plane (items of bf16 tables): there the weights are the differences (a p - the targets') themselves, so one plane rounds
-// each by at most 2^-11 of itself, an eighth of what the gradient's own rounding does, and a third of the pass's instructions
-// goes (8192 rows x 100,000 items K = 256 1386 -> 1267 us, now 1225).  Rows' weights are p alone, and the targets come off
-// later: one plane would leave 2^-11 of p where p nearly equals the target, so they have two; so has fp16, whose
-// gradients hold 11 bits themselves.
+// The weights have two planes whatever the tables' type: with one, 2^-11 of each weight, 6 of 100 numbers of a bf16
+// gradient are rounded to the neighbour of the nearest.
 // The matrix instructions bound rows over items (1.16 PFLOP/s of them at K = 128 fp32, 1.14 at K = 256 bf16; a large
 // library product reaches 1.2), so the loop keeps them fed: the next tile's scores are made beside the exponentials of this one's,
-// the sums beside the rounding.  Items over rows have the records and the shares besides (K = 128 fp32 385 / 510 us), and
-// with one plane fewer matrix instructions to hide 85 others a tile behind (K = 128 bf16 0.67 PFLOP/s).  The tiles' way
-// from L2 is a seventh to a fifth of it: 8 wavefronts a workgroup, which halve that, 320 / 360 us for 331 / 316; two own tiles a
+// the sums beside the rounding.  Items over rows have the records and the shares besides (K = 128 fp32 385 / 510 us).  The
+// tiles' way from L2 is a seventh to a fifth of it: 8 wavefronts a workgroup, which halve that, 320 / 360 us for 331 / 316; two own tiles a
 // wavefront, which halve the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
-template <int NP, int KC, int DB, bool COL, bool one_plane>
+template <int NP, int KC, int DB, bool COL>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
   constexpr int KD = KC / 2;
@@ -792,14 +788,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       for (int i = 0; i < TA && i < 2 * DB; ++i) read_turned(g[i], t, i);
       u32x4 ph[2], pl[2];
       auto make_planes = [&](int k, int i) {
-        if constexpr (one_plane) {
-          ph[k][i] = to_halves(p[8 * k + 2 * i], p[8 * k + 2 * i + 1]);
-        } else {
-          uint32_t h, l;
-          planes(p[8 * k + 2 * i], p[8 * k + 2 * i + 1], h, l);
-          ph[k][i] = h;
-          pl[k][i] = l;
-        }
+        uint32_t h, l;
+        planes(p[8 * k + 2 * i], p[8 * k + 2 * i + 1], h, l);
+        ph[k][i] = h;
+        pl[k][i] = l;
       };
 #pragma unroll
       for (int i = 0; i < 4; ++i) make_planes(0, i);
@@ -816,7 +808,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
           for (int z = 2 * i / DB + 1; z <= 2 * (i + 1) / DB && z < 4; ++z) v[z] = row_values(t + 1, z, 0);
         }
         o[b] = mfma(g[i][0], halves(ph[k]), o[b]);
-        if constexpr (!one_plane) o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
+        o[b] = mfma(g[i][0], halves(pl[k]), o[b]);
         if constexpr (NP == 2) o[b] = mfma(g[i][1], halves(ph[k]), o[b]);
         if (k == 0) {
 #pragma unroll
@@ -2238,37 +2230,34 @@ void hip_launch(void (*f)(PassArgs), dim3 grid, unsigned lds, const PassArgs &a,
 }
 
 template <int NP, int KC, int DB>
-void launch_pass(const PassArgs &a, bool col, bool one_plane, hipStream_t s) {
+void launch_pass(const PassArgs &a, bool col, hipStream_t s) {
   const dim3 grid = grid_of(up(a.own_tiles, kWaves) * a.splits);
   const unsigned lds = static_cast<unsigned>(stage_of(NP, KC, DB, col).halves * 2);
   if (!col) {
-    hip_launch((k_pass<NP, KC, DB, false, false>), grid, lds, a, s);
+    hip_launch((k_pass<NP, KC, DB, false>), grid, lds, a, s);
   } else if constexpr (DB > 0) {
-    if constexpr (NP == 1) {
-      if (one_plane) return hip_launch((k_pass<NP, KC, DB, true, true>), grid, lds, a, s);
-    }
-    hip_launch((k_pass<NP, KC, DB, true, false>), grid, lds, a, s);
+    hip_launch((k_pass<NP, KC, DB, true>), grid, lds, a, s);
   }
 }
 
 template <int NP, int KC>
-void run_pass_of(PassArgs a, bool col, bool sums, bool one_plane, hipStream_t s) {
+void run_pass_of(PassArgs a, bool col, bool sums, hipStream_t s) {
   constexpr int KD = KC / 2, DB = std::min(KD, 8);
   a.d0 = 0;
-  if (!sums) launch_pass<NP, KC, 0>(a, false, false, s);
+  if (!sums) launch_pass<NP, KC, 0>(a, false, s);
   else
-    for (; a.d0 < KD; a.d0 += DB) launch_pass<NP, KC, DB>(a, col, one_plane, s);
+    for (; a.d0 < KD; a.d0 += DB) launch_pass<NP, KC, DB>(a, col, s);
 }
 template <int NP>
-void run_pass(const PassArgs &a, int k16, bool col, bool sums, bool one_plane, hipStream_t s) {
+void run_pass(const PassArgs &a, int k16, bool col, bool sums, hipStream_t s) {
   switch (k16) {
-    case 2: return run_pass_of<NP, 2>(a, col, sums, one_plane, s);
-    case 4: return run_pass_of<NP, 4>(a, col, sums, one_plane, s);
-    case 6: return run_pass_of<NP, 6>(a, col, sums, one_plane, s);
-    case 8: return run_pass_of<NP, 8>(a, col, sums, one_plane, s);
-    case 12: return run_pass_of<NP, 12>(a, col, sums, one_plane, s);
-    case 16: return run_pass_of<NP, 16>(a, col, sums, one_plane, s);
-    default: return run_pass_of<NP, 32>(a, col, sums, one_plane, s);
+    case 2: return run_pass_of<NP, 2>(a, col, sums, s);
+    case 4: return run_pass_of<NP, 4>(a, col, sums, s);
+    case 6: return run_pass_of<NP, 6>(a, col, sums, s);
+    case 8: return run_pass_of<NP, 8>(a, col, sums, s);
+    case 12: return run_pass_of<NP, 12>(a, col, sums, s);
+    case 16: return run_pass_of<NP, 16>(a, col, sums, s);
+    default: return run_pass_of<NP, 32>(a, col, sums, s);
   }
 }
 
@@ -2352,7 +2341,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       a.scal = scal;
       a.scale = scale;
       a.tiles_per_split = p.rper;
-      run_pass<NP>(a, p.k16, false, dx, false, s);
+      run_pass<NP>(a, p.k16, false, dx, s);
     }
     RowArgs<T> r{};
     r.t = t;
@@ -2405,7 +2394,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
       a.tiles_per_split = p.cper;
       a.first = t.entries > 0 ? first : nullptr;
       a.pay = rec[from].pay;
-      run_pass<NP>(a, p.k16, true, true, std::is_same<T, bf16_t>::value, s);
+      run_pass<NP>(a, p.k16, true, true, s);
     }
   }
   if (dw) {
