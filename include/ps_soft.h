@@ -40,8 +40,10 @@
  *     keeps every workspace until it is destroyed;
  *   - a handle is not thread-safe, and calls on one handle, replays of graphs that hold its
  *     calls among them, must not overlap: they share the workspace.  Use a handle each;
- *   - the losses scale each table by a power of two and round its numbers (fp32: to 22 bits; those
- *     below 2^-28 of the table's largest finite number: to 2^-38 of that one);
+ *   - the losses scale each table by a power of two and round its numbers: fp32 to 22 bits, but to no
+ *     less than 2^-38 of the table's largest finite number (felt below 2^-16 of it; bf16 and f16
+ *     numbers are exact above 2^-28 of it).  The softmax's weights have 22 bits, those of a row or of an
+ *     item that are far below its largest to 2^-31 of that one;
  *   - equal calls give equal bits: sums have a fixed order, whatever runs beside them.
  */
 #ifndef PS_SOFT_H

@@ -49,6 +49,7 @@ constexpr float kNone = -1e30f; // reference before the first tile: finite, so t
 // p' = 2^(score - reference + kShift), and the reference follows the maximum when it is exceeded by more than
 // kLag: p' stays below 2^15, and a weight of 2^-17 of the largest keeps 22 bits
 constexpr float kShift = 7.f, kLag = 8.f;
+constexpr float kFar = -120.f;  // least reference of an item with targets: 2^(kShift - reference) is a finite number
 
 // A launch holds less than 2^32 threads in a dimension: workgroups beyond 2^22 go to the second
 constexpr int kGridBits = 22;
@@ -310,7 +311,7 @@ __device__ inline int scale_exp(float most) {
 // Scalars that the kernels share
 struct Scal {
   int32_t ex, ew;  // x~ = x 2^ex, w~ = w 2^ew
-  float amax;      // a power of two >= 2 |gw| sum |coef| of every row (1 where all are 0)
+  float amax;      // a power of two >= 2 |gw| sum |coef| of every row (1 where all are 0): shares and targets are taken by it
   float pad;
 };
 
@@ -401,7 +402,7 @@ struct PassArgs {
   int64_t own_tiles, str_rows;
   int32_t d0;                      // the first block of 32 numbers summed here
   int32_t splits;                  // pieces of the stream
-  const float *rowvec;             // COL: per tile of 32 stream rows, 32 times minus the log2-sum-exp, and 32 shares
+  const float *rowvec;             // COL: per tile of 32 stream rows, 32 powers of two and 32 factors (see k_row_finish)
   const Scal *scal;
   float scale;                     // log2(e) / tau
   int64_t tiles_per_split;
@@ -517,6 +518,12 @@ __device__ inline int64_t first_of_row(const uint2 *pay, int64_t b, int64_t e, u
   return b;
 }
 
+// The largest of the two lanes that hold an own row
+__device__ inline float of_both_halves(float v) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // Wavefronts per SIMD that the registers are cut for
 constexpr int waves_per_simd(int np, int kc, int db) {
   const int need = 4 * kc * np + 16 * db;  // own rows and sums; a tile's scores, weights and fragments take 60 to 110 more
@@ -531,7 +538,7 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // gradient are rounded to the neighbour of the nearest.
 // The matrix instructions bound rows over items (1.16 PFLOP/s of them at K = 128 fp32, 1.14 at K = 256 bf16; a large
 // library product reaches 1.2), so the loop keeps them fed: the next tile's scores are made beside the exponentials of this one's,
-// the sums beside the rounding.  Items over rows have the records and the shares besides (K = 128 fp32 385 / 510 us).  The
+// the sums beside the rounding.  Items over rows have the records and the factors besides (K = 128 fp32 385 / 510 us).  The
 // tiles' way from L2 is a seventh to a fifth of it: 8 wavefronts a workgroup, which halve that, 320 / 360 us for 331 / 316; two own tiles a
 // wavefront, which halve the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
 template <int NP, int KC, int DB, bool COL>
@@ -587,9 +594,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   for (int b = 0; b < DB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-  // Rows of an own tile with targets are the softmax's weights less the targets', which are of size 1 whatever the softmax's
-  // are: the reference stays at -kLag (weights <= 1), and small weights keep 2^-25 of 2^15.  Elsewhere it
-  // follows the largest weight.
+  // The reference of each own row follows the largest of its own weights, an item's targets among them: so an item of
+  // small weights keeps 22 bits of them, whatever its neighbours' or the rows' shares are.
   float ref = kNone, sum = 0.f, lost = 0.f, unit = 0.f;
   bool targets = false;
   Window win;
@@ -604,10 +610,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       win.open(a.pay, b, e, lane);
       targets = win.due < static_cast<uint32_t>(t1) * kTile;
     }
-    if (targets) {
-      ref = -kLag;
-      unit = ldexpf(1.f / a.scal->amax, static_cast<int>(kShift + kLag));
-    }
+    unit = 1.f / a.scal->amax;
   }
   // Chunk c of a tile's score fragments, and step i of its turned ones (half i / DB, block i % DB)
   auto read_scores = [&](h8 (&f)[NP], int t, int c) {
@@ -628,9 +631,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
     }
     return s;
   };
-  // log2 weights of stream rows r: the score's, less the row's log-sum-exp where it is known.  That is subtracted here: as
-  // the matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
-  auto row_values = [&](int t, int g, int which) {  // rows 8g + 4h ..+3: minus the log-sum-exps, or the shares
+  // log2 weights of stream rows r: the score's, and the row's power of two.  That is added here: as the matrix
+  // instruction's first value, every one of its roundings would be at the size of the log-sum-exp
+  auto row_values = [&](int t, int g, int which) {  // rows 8g + 4h ..+3: the powers of two, or the factors
     return *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(buf + sg.at_rows + (t & 3) * 128) + which * 32 + g * 8 + half * 4);
   };
   fetch_scores(t0);
@@ -693,25 +696,22 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
         top = fmaxf(top, p[r]);
       }
     }
-    if (!COL || !targets) {
-      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-      top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-      if (__any(top > ref + kLag)) {
-        const float to = top > ref + kLag ? top : ref;
-        const float down = __builtin_amdgcn_exp2f(ref - to);
-        ref = to;
-        sum *= down;
-        lost *= down;
+    top = of_both_halves(top);
+    if (__any(top > ref + kLag)) {
+      const float to = top > ref + kLag ? top : ref;
+      const float down = __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      sum *= down;
+      lost *= down;
 #pragma unroll
-        for (int b = 0; b < DB; ++b)
+      for (int b = 0; b < DB; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[b][r] *= down;
-      }
+        for (int r = 0; r < 16; ++r) o[b][r] *= down;
     }
     const float shift = kShift - ref;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
-    f32x4 share[4];  // each read a step ahead of its use
-    if constexpr (COL) share[0] = row_values(t, 0, 1);
+    f32x4 factor[4];  // each read a step ahead of its use
+    if constexpr (COL) factor[0] = row_values(t, 0, 1);
     // the next tile's scores beside this one's weights (behind the last tile: what lies in LDS, and not used)
     f32x16 next;
 #pragma unroll
@@ -722,13 +722,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       if (c + SA < KC) read_scores(f[c + SA], t + 1, c + SA);
       if constexpr (COL) {
 #pragma unroll
-        for (int g = 4 * c / KC + 1; g <= 4 * (c + 1) / KC && g < 4; ++g) share[g] = row_values(t, g, 1);
+        for (int g = 4 * c / KC + 1; g <= 4 * (c + 1) / KC && g < 4; ++g) factor[g] = row_values(t, g, 1);
       }
       next = add_scores(next, f[c], c);
 #pragma unroll
       for (int r = 16 * c / KC; r < 16 * (c + 1) / KC; ++r) {
         p[r] = __builtin_amdgcn_exp2f(p[r] + shift);
-        if constexpr (COL) p[r] *= share[r >> 2][r & 3];
+        if constexpr (COL) p[r] *= factor[r >> 2][r & 3];
         else w[r & 3] += p[r];
         asm volatile("" : "+v"(p[r]));  // here, beside the matrix instructions
       }
@@ -774,10 +774,28 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
             __builtin_amdgcn_wave_barrier();
             *y0 = *y1 = f32x4{0.f, 0.f, 0.f, 0.f};
             __builtin_amdgcn_wave_barrier();
+            // as the weights', and half of their room: the two together stay below 2^15 + 2^14
+            float big = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fabsf(v0[i]), fabsf(v1[i])));
+            big = of_both_halves(big);
+            float to = big > 0.f ? fmaxf(ref, kFar) : ref;
+            if (big > __builtin_amdgcn_exp2f(to + (kLag - 1.f))) to = __builtin_amdgcn_logf(big);
+            if (__any(to != ref)) {
+              const float down = __builtin_amdgcn_exp2f(ref - to);
+              ref = to;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) p[r] *= down;
+#pragma unroll
+              for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[b][r] *= down;
+            }
+            const float up = __builtin_amdgcn_exp2f(fminf(kShift - ref, kShift - kFar));  // lanes without targets: any finite number
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              p[8 * k + i] -= v0[i];
-              p[8 * k + 4 + i] -= v1[i];
+              p[8 * k + i] = fmaf(-up, v0[i], p[8 * k + i]);
+              p[8 * k + 4 + i] = fmaf(-up, v1[i], p[8 * k + 4 + i]);
             }
           }
         }
@@ -905,9 +923,8 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   const float mine = top;
   top = wave_max(top);
   den = wave_sum(den * __builtin_amdgcn_exp2f(mine - top));
-  // in 64 bits: the loss is what is left of total lse - x . c, and lse2 in 32 would be off by 5e-7 at 8 .. 16
-  const double lse64 = static_cast<double>(top - kShift) + log2(static_cast<double>(den)), lse = lse64 * 0.69314718055994530942;
-  const float lse2 = static_cast<float>(lse64);
+  // in 64 bits: the loss is what is left of total lse - x . c, and a log2-sum-exp in 32 would be off by 5e-7 at 8 .. 16
+  const double lse64 = static_cast<double>(top) - static_cast<double>(kShift) + log2(static_cast<double>(den)), lse = lse64 * 0.69314718055994530942;
   f32x4 acc[V], o[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1008,8 +1025,14 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
       a.loss[i] = act || a.t.extra[i] != 0.f ? static_cast<float>(a.t.tau * a.t.tau * (a.t.extra[i] + (a.t.total[i] * lse - d / a.t.tau))) : 0.f;
     if (a.lse) a.lse[i] = static_cast<float>(lse);
     if (a.rowvec) {
-      a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? -lse2 : -__builtin_inff();
-      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = act ? a.t.share[i] / a.scal->amax : 0.f;
+      // a p_ij = 2^(score + v) f with the share a = 2^e m: v = e - log2-sum-exp, so that the items' references see the share
+      // too, and f = m 2^r makes up for the rounding of v by r (at most 2^-19 at 16 .. 32)
+      int e;
+      const float m = frexpf(act ? a.t.share[i] / a.scal->amax : 0.f, &e);
+      const double v = (m == 0.f ? -__builtin_inf() : static_cast<double>(e)) - lse64;
+      const float v32 = static_cast<float>(v);
+      a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? v32 : -__builtin_inff();
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = m == 0.f ? 0.f : m * static_cast<float>(1.0 + (v - v32) * 0.69314718055994530942);
     }
   }
   if (a.dX && lane < G) {

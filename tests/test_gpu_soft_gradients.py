@@ -68,3 +68,118 @@ def test_item_gradients_are_rounded_once(soft, n, M, K, splits, dtype):
                 most = off(got[q], v[q], b[q], dtype)
                 say(f"{name} n={n} M={M} K={K} {dtype} {part}: {most:.3f} of its bound")
                 assert most <= 1, (name, part, most)
+
+
+def item_gradients(x, w, y, weight, tau=1.0):
+    """dW in 64 bits, and what fp32 sums of weights in two planes may be off, item by item: scores, log-sum-exps and
+    exponentials as in soft_ref, and each weight 2^-25 where the item's own largest one is at least 2^6."""
+    n, K = x.shape
+    M = w.shape[0]
+    U = soft_ref.U
+    s, a = x @ w.T / tau, np.abs(x) @ np.abs(w).T / tau
+    top = s.max(1, keepdims=True)
+    lse = np.log(np.exp(s - top).sum(1, keepdims=True)) + top
+    g = (weight * tau)[:, None]
+    soft = g * y.sum(1, keepdims=True) * np.exp(s - lse)
+    want = (soft - g * y).T @ x
+    es = (K + 16) * 2 * U * a
+    ep = es + es.max(1, keepdims=True) + (M + 64) * U + 4 * U * np.abs(lse) + 2.0 ** -20 + (M + n + 64) * U
+    ey = (n + M + 16) * U
+    bound = (np.abs(soft) * ep + np.abs(g * y) * ey).T @ np.abs(x)
+    largest = np.maximum(np.abs(soft), np.abs(g * y)).max(0)
+    bound += 2.0 ** -31 * largest[:, None] * np.abs(x).sum(0) + 2.0 ** -37 * (np.abs(soft) + np.abs(g * y)).sum(0)[:, None] * np.abs(x).max()
+    return want, bound
+
+
+@pytest.mark.parametrize("splits", [0, 3])
+@pytest.mark.parametrize("dtype,depth", [(F32, 10), (F32, 20), (F32, 28), (F32, 60), (BF16, 20), (BF16, 28), (BF16, 60), (F16, 10)])
+def test_improbable_items_beside_targets(soft, dtype, depth, splits):
+    # every other item has probabilities of e^-depth of its neighbours', which are targets: their gradients keep their digits
+    n, M, K = 300, 64, 4
+    X, W, g = tables(n, M, K, dtype, depth)
+    X[:, 0] = 4
+    W[:, 0] = -(torch.arange(M) % 2).to(dtype).cuda() * depth / 4
+    item = (torch.randint(0, M // 2, (n,), generator=g, dtype=torch.int32) * 2).cuda()
+    y = np.zeros((n, M))
+    y[np.arange(n), item.cpu()] = 1
+    want, bound = item_gradients(soft_ref.f64(X), soft_ref.f64(W), y, np.ones(n))
+    with soft.PsSoft(M, K, dtype, splits=splits) as h:
+        most = off(h.xent(X, W, item)[3], want, bound, dtype)
+    say(f"improbable e^-{depth} {dtype} splits={splits}: {most:.3f} of its bound")
+    assert most <= 1
+
+
+@pytest.mark.parametrize("power", [10, 20, 40])
+def test_one_heavy_row(soft, power):
+    # a row of weight 2^power that only knows one item: the other items' gradients are the light rows'
+    n, M, K = 200, 100, 8
+    X, W, g = tables(n, M, K, F32, power)
+    W[:, 0] = 0
+    W[33, 0] = 32
+    X[:, 0] = 0
+    X[50] = 0
+    X[50, 0] = 4
+    item = torch.randint(0, M, (n,), generator=g, dtype=torch.int32)
+    item[50] = 33
+    weight = torch.ones(n)
+    weight[50] = 2.0 ** power
+    y = np.zeros((n, M))
+    y[np.arange(n), item] = 1
+    want, bound = item_gradients(soft_ref.f64(X), soft_ref.f64(W), y, weight.numpy().astype(np.float64))
+    with soft.PsSoft(M, K) as h:
+        most = off(h.xent(X, W, item.cuda(), weight=weight.cuda())[3], want, bound, F32)
+    say(f"heavy row 2^{power}: {most:.3f} of its bound")
+    assert most <= 1
+
+
+@pytest.mark.parametrize("splits", [0, 1, 4])
+@pytest.mark.parametrize("spread", [0, 12, 60])
+def test_shares_and_values_of_either_sign_and_far_sizes(soft, spread, splits):
+    # rows whose values add up to something negative or to nothing, weights of either sign over 2^spread, a row after another
+    # growing or shrinking, items twice in a list, values of 0
+    n, M, K = 260, 97, 12
+    X, W, g = tables(n, M, K, F32, spread + 1)
+    value = torch.randn(n, 6, generator=g)
+    value[:, 5] = -value[:, :5].sum(1) * (torch.arange(n) % 3 == 0)
+    value[::7, 2] = 0
+    item = torch.randint(0, M, (n, 6), generator=g, dtype=torch.int32)
+    item[::5, 1] = item[::5, 0]
+    e = torch.rand(n, generator=g) * spread
+    e[:100] = e[:100].sort().values  # rows that grow, and rows that shrink
+    e[100:200] = e[100:200].sort(descending=True).values
+    weight = torch.exp2(e) * torch.where(torch.rand(n, generator=g) < 0.5, -1.0, 1.0)
+    y = np.zeros((n, M))
+    np.add.at(y, (np.arange(n)[:, None], item.numpy()), soft_ref.f64(value))
+    wt = soft_ref.f64(weight)
+    want, bound = item_gradients(soft_ref.f64(X), soft_ref.f64(W), y, wt)
+    # a sum of six fp32 values is off by 6 u of the values', where they cancel
+    sizes = soft_ref.f64(value.abs()).sum(1)
+    p = np.exp(soft_ref.f64(X) @ soft_ref.f64(W).T)
+    p /= p.sum(1, keepdims=True)
+    ya = np.zeros((n, M))
+    np.add.at(ya, (np.arange(n)[:, None], item.numpy()), soft_ref.f64(value.abs()))
+    bound += 6 * soft_ref.U * (np.abs(wt)[:, None] * (sizes[:, None] * p + 2 * ya)).T @ np.abs(soft_ref.f64(X))
+    ptr = torch.arange(0, 6 * n + 1, 6).cuda()
+    with soft.PsSoft(M, K, splits=splits) as h:
+        got = h.xent(X, W, item.flatten().cuda(), row_ptr=ptr, value=value.flatten().cuda(), weight=weight.cuda())[3]
+        again = h.xent(X, W, item.flatten().cuda(), row_ptr=ptr, value=value.flatten().cuda(), weight=weight.cuda(), grad="W")[3]
+    most = off(got, want, bound, F32)
+    say(f"shares over 2^{spread} splits={splits}: {most:.3f} of its bound")
+    assert most <= 1 and torch.equal(got, again)
+
+
+def test_tiny_and_huge_weights(soft):
+    # all rows' weights scaled by a power of two scale the gradients exactly; the smallest and the largest of them together
+    n, M, K = 70, 80, 10
+    X, W, g = tables(n, M, K, F32, 5)
+    item = torch.randint(0, M, (n,), generator=g, dtype=torch.int32).cuda()
+    weight = torch.randn(n, generator=g).cuda()
+    with soft.PsSoft(M, K) as h:
+        base = h.xent(X, W, item, weight=weight)
+        for e in (-90, -40, 30, 100):
+            far = h.xent(X, W, item, weight=weight * 2.0 ** e)
+            assert torch.equal(far[2] * 2.0 ** -e, base[2]) and torch.equal(far[3] * 2.0 ** -e, base[3]), e
+        weight[::2] *= 2.0 ** -120
+        weight[1] = 2.0 ** 100
+        out = h.xent(X, W, item, weight=weight)
+        assert all(torch.isfinite(t).all() for t in out)
