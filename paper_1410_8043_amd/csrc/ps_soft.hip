@@ -141,13 +141,19 @@ struct Targets {
   const float *score, *tlse; // distill
   int64_t ldt;
   float tau;
+  double per_tau;            // 1 / tau
   const float *weight;
   int32_t *key;              // NULL: no dW
   uint2 *pay;
   int32_t *act;                             // [n] 0: masked
-  float *total, *extra, *share, *gw, *logz; // [n] sum of coef; sum q log q (NaN: a bad row); gw total; weight tau; the teacher's log-sum-exp
+  float *total, *extra, *share, *gw;        // [n] sum of coef; sum q log q (NaN: a bad row); gw total; weight tau
+  double *logz;                             // [n] the teacher's log-sum-exp
   float *part;                              // [gridDim.x] largest |gw| sum |coef|
 };
+
+// log q of a teacher's score, z the log-sum-exp over tau.  In 64 bits: both may be far larger than their difference (scores
+// of 3000 in fp32 put q off by 1e-4)
+__device__ inline float log_q(const Targets &a, float score, double z) { return static_cast<float>(fma(static_cast<double>(score), a.per_tau, -z)); }
 
 __device__ inline bool row_range(const int64_t *row_ptr, int64_t entries, int32_t k, int64_t i, int64_t &b, int64_t &e) {
   if (!row_ptr) {
@@ -183,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
     bool bad = !row_range(a.row_ptr, a.entries, a.k, i, b, e);
     const int64_t src = Distill ? i * a.ldt - b : 0;  // the lists' stride
     const float w = a.weight ? a.weight[i] : 1.f;
-    float z = 0.f;  // log of the teacher's sum
+    double z = 0.0;  // log of the teacher's sum
     if constexpr (Distill) {
       bool some = false;
       float top = -inf;
@@ -192,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
         const float t = j >= 0 && j < a.items ? a.score[x + src] : -inf;
         if (!(t == -inf)) {
           some = true;
-          top = t != t ? t : fmaxf(top, t / a.tau);
+          top = t != t ? t : fmaxf(top, t);
         }
       }
       if (__any(some)) {
@@ -204,9 +210,9 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
           for (int64_t x = b + lane; x < e; x += 64) {
             const int32_t j = a.item[x + src];
             const float t = j >= 0 && j < a.items ? a.score[x + src] : -inf;
-            if (!(t == -inf)) den += expf(t / a.tau - top);
+            if (!(t == -inf)) den += expf(log_q(a, t, top * a.per_tau));
           }
-          z = top + logf(wave_sum(den));
+          z = top * a.per_tau + log(static_cast<double>(wave_sum(den)));
         }
       }
     }
@@ -222,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_targets(Targets a) {
         if constexpr (Distill) {
           const float t = a.score[x + src];
           here = !(t == -inf);
-          const float lq = t / a.tau - z;
+          const float lq = log_q(a, t, z);
           c = here ? expf(lq) : 0.f;
           extra += c == 0.f ? 0.f : c * lq;
         } else {
@@ -932,7 +938,7 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     int64_t b, e;
     row_range(a.t.row_ptr, a.t.entries, a.t.k, i, b, e);
     const int64_t src = a.t.score ? i * a.t.ldt - b : 0;
-    const float z = a.t.score ? a.t.logz[i] : 0.f;
+    const double z = a.t.score ? a.t.logz[i] : 0.0;
     int32_t key[RF], coming[RF];
     float c[RF], soon[RF];
     auto read_list = [&](int64_t q) {  // a round ahead: its items' rows wait for it
@@ -958,7 +964,7 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
 #pragma unroll
       for (int f = 0; f < RF; ++f) {
         if (a.t.score) {
-          c[f] = key[f] >= 0 ? expf(c[f] / a.t.tau - z) : 0.f;
+          c[f] = key[f] >= 0 ? expf(log_q(a.t, c[f], z)) : 0.f;
           if (c[f] == 0.f) continue;  // no entry: what its item holds does not count
         }
 #pragma unroll
@@ -2223,7 +2229,7 @@ Plan plan(const ps_soft_t *h, int64_t n, int64_t entries, bool dx, bool dw, bool
   p.extra = a.take(n * 4);
   p.share = a.take(n * 4);
   p.gw = a.take(n * 4);
-  p.logz = a.take(n * 4);
+  p.logz = a.take(n * 8);
   p.row_part = a.take(kRowParts * 4);
   p.part = a.take(2 * kParts * 4);
   p.scal = a.take(sizeof(Scal));
@@ -2327,7 +2333,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
   t.extra = at_f(p.extra);
   t.share = at_f(p.share);
   t.gw = at_f(p.gw);
-  t.logz = at_f(p.logz);
+  t.logz = reinterpret_cast<double *>(base + p.logz);
   t.part = at_f(p.row_part);
   Table<T> x{X, ldx, t.n, aligned4(X, ldx), t.act}, w{W, ldw, h->items, aligned4(W, ldw), nullptr};
   _Float16 *px = reinterpret_cast<_Float16 *>(base + p.px), *pw = reinterpret_cast<_Float16 *>(base + p.pw);
@@ -2745,6 +2751,7 @@ int ps_soft_xent(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const void
   t.item = item;
   t.value = value;
   t.tau = 1.f;
+  t.per_tau = 1.0;
   t.weight = weight;
   return any_loss<false>(h, t, X, ldx, W, ldw, loss, lse, dX, lddx, dW, lddw);
 }
@@ -2768,6 +2775,7 @@ int ps_soft_distill(ps_soft_t *h, int64_t n, const void *X, int64_t ldx, const v
   t.tlse = tlse;
   t.ldt = ldt;
   t.tau = tau;
+  t.per_tau = 1.0 / tau;
   t.weight = weight;
   return any_loss<true>(h, t, X, ldx, W, ldw, loss, lse, dX, lddx, dW, lddw);
 }

@@ -1,4 +1,4 @@
-"""ps_soft's item gradients on the device, number by number, against 64 bits.
+"""ps_soft's item gradients on the device, number by number, and its teachers' scores, against 64 bits.
 
 Bounds: those of soft_ref for fp32 tables, whatever the tables' type (scores, weights in two planes of 11 bits,
 sums), and one rounding to the gradient's type: half of its step at the number's own size.
@@ -183,3 +183,27 @@ def test_tiny_and_huge_weights(soft):
         weight[1] = 2.0 ** 100
         out = h.xent(X, W, item, weight=weight)
         assert all(torch.isfinite(t).all() for t in out)
+
+
+@pytest.mark.parametrize("tau,full", [(1.0, False), (0.75, False), (3.3, False), (2.0, True), (0.5, True)])
+@pytest.mark.parametrize("far", [300, -3000, 30_000])
+def test_teachers_of_far_scores(soft, far, tau, full):
+    # a number added to all of a teacher's scores changes nothing: the sums are exact here (multiples of 2^-8 below 2^15), so the
+    # bounds are those of the scores without it
+    n, M, K, k = 70, 300, 16, 20
+    X, W, g = tables(n, M, K, F32, far % 97)
+    score = (torch.randn(n, k, generator=g) * 512).round() / 256
+    score[3, 5:] = -float("inf")
+    ids = torch.stack([torch.randperm(M, generator=g)[:k] for _ in range(n)]).int()
+    ids[4] = -1
+    ids, score = ids.cuda(), score.cuda()
+    tlse = (torch.logsumexp(score / tau, 1) * 256 + 100).round() / 256 if full else None
+    weight = torch.rand(n, generator=g).cuda()
+    want, bounds = soft_ref.distill(X, W, ids, score, tau, tlse, weight)
+    with soft.PsSoft(M, K) as h:
+        got = h.distill(X, W, ids, score + far, tau=tau, tlse=None if tlse is None else tlse + far / tau, weight=weight)
+        only = h.distill(X, W, ids, score + far, tau=tau, tlse=None if tlse is None else tlse + far / tau, weight=weight, grad=False)
+    for part, a, v, b in zip(("loss", "lse", "dX", "dW", "loss alone", "lse alone"), (*got, *only), (*want, *want[:2]), (*bounds, *bounds[:2])):
+        most = soft_ref.near(a, v, b)
+        say(f"teacher far={far} tau={tau} full={full} {part}: {most:.3f} of its bound")
+        assert most <= 1, part
