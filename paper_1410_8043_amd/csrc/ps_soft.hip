@@ -1028,7 +1028,7 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
   }
   if (lane == 0) {
     if (a.loss)
-      a.loss[i] = act || a.t.extra[i] != 0.f ? static_cast<float>(a.t.tau * a.t.tau * (a.t.extra[i] + (a.t.total[i] * lse - d / a.t.tau))) : 0.f;
+      a.loss[i] = act || a.t.extra[i] != 0.f ? static_cast<float>(static_cast<double>(a.t.tau) * a.t.tau * (a.t.extra[i] + (a.t.total[i] * lse - d / a.t.tau))) : 0.f;
     if (a.lse) a.lse[i] = static_cast<float>(lse);
     if (a.rowvec) {
       // a p_ij = 2^(score + v) f with the share a = 2^e m: v = e - log2-sum-exp, so that the items' references see the share

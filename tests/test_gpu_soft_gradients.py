@@ -207,3 +207,25 @@ def test_teachers_of_far_scores(soft, far, tau, full):
         most = soft_ref.near(a, v, b)
         say(f"teacher far={far} tau={tau} full={full} {part}: {most:.3f} of its bound")
         assert most <= 1, part
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("power", [-24, -80, -100])
+def test_temperatures_whose_square_is_out_of_range(soft, power, few):
+    # at a temperature near 0 both softmaxes are one item, and loss = tau (the student's best score - its score of the teacher's
+    # item): about tau, where tau^2 in fp32 would be 0.  tau a power of two: scores / tau are exact
+    n, M, K, k = 40, 200, 8, 5
+    X, W, g = tables(n, M, K, F32, 3)
+    ids = torch.stack([torch.randperm(M, generator=g)[:k] for _ in range(n)]).int().cuda()
+    score = torch.randn(n, k, generator=g).cuda()
+    tau = 2.0 ** power
+    with soft.PsSoft(M, K, splits=0 if few else 2) as h:
+        loss = soft_ref.f64(h.distill(X, W, ids, score, tau=tau, grad=not few)[0])
+    s = soft_ref.f64(X) @ soft_ref.f64(W).T
+    want = s.max(1) - s[np.arange(n), soft_ref.f64(ids.gather(1, score.argmax(1, keepdim=True)))[:, 0].astype(int)]
+    # scores in fp32 as in soft_ref; ties of the best within tau add at most log M
+    a = np.abs(soft_ref.f64(X)) @ np.abs(soft_ref.f64(W)).T
+    bound = ((K + 16) * 4 + 8) * soft_ref.U * a.max(1) + tau * np.log(M) * 2
+    most = float((np.abs(loss / tau - want) / bound).max())
+    say(f"tau=2^{power} few={few}: {most:.3f} of its bound")
+    assert most <= 1
