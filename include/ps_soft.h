@@ -44,6 +44,8 @@
  *     less than 2^-38 of the table's largest finite number (felt below 2^-16 of it; bf16 and f16
  *     numbers are exact above 2^-28 of it).  The softmax's weights have 22 bits, those of a row or of an
  *     item that are far below its largest to 2^-31 of that one;
+ *     A score is off by about 2^-22 of sum |x_k w_k|: where that is no longer small against 1 (scores
+ *     beyond 10^5), gradients lose their digits, and dW its meaning (beyond 10^7);
  *   - equal calls give equal bits: sums have a fixed order, whatever runs beside them.
  */
 #ifndef PS_SOFT_H

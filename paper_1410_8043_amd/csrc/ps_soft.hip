@@ -45,7 +45,7 @@ constexpr int kThreads = 256;
 constexpr int kPackBlocks = 8;  // blocks of 32 numbers that packing holds in LDS at once
 constexpr int kParts = 256;     // workgroups, and partial maxima, of each table's scan
 constexpr int kRowParts = 4096; // most workgroups, and partial maxima, of the row scan
-constexpr float kNone = -1e30f; // reference before the first tile: finite, so that 2^(-inf - kNone) is 0
+constexpr float kNone = -3e38f; // reference before the first tile: below all scores, and finite, so that 2^(-inf - kNone) is 0
 // p' = 2^(score - reference + kShift), and the reference follows the maximum when it is exceeded by more than
 // kLag: p' stays below 2^15, and a weight of 2^-17 of the largest keeps 22 bits
 constexpr float kShift = 7.f, kLag = 8.f;
@@ -1038,7 +1038,8 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
       const double v = (m == 0.f ? -__builtin_inf() : static_cast<double>(e)) - lse64;
       const float v32 = static_cast<float>(v);
       a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? v32 : -__builtin_inff();
-      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = m == 0.f ? 0.f : m * static_cast<float>(1.0 + (v - v32) * 0.69314718055994530942);
+      const double rest = (v - v32) * 0.69314718055994530942;  // below 2^-9 for scores below 2^15
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = m == 0.f ? 0.f : m * static_cast<float>(1.0 + rest * (1.0 + 0.5 * rest));
     }
   }
   if (a.dX && lane < G) {

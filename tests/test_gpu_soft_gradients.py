@@ -229,3 +229,25 @@ def test_temperatures_whose_square_is_out_of_range(soft, power, few):
     most = float((np.abs(loss / tau - want) / bound).max())
     say(f"tau=2^{power} few={few}: {most:.3f} of its bound")
     assert most <= 1
+
+
+@pytest.mark.parametrize("splits,grad", [(0, False), (0, True), (3, True)])
+def test_scores_far_below_zero(soft, splits, grad):
+    # every score of a row near -2^110: one item takes all, lse is its score, the loss what the target is below it
+    n, M, K = 33, 90, 4
+    X, W, g = tables(n, M, K, F32, 9)
+    X, W = X.abs() + 1, -(W.abs() + 1)
+    W[:, 0] -= torch.arange(M).cuda()
+    X, W = X * 2.0 ** 55, W * 2.0 ** 55
+    item = torch.randint(0, M, (n,), generator=g, dtype=torch.int32).cuda()
+    s = soft_ref.f64(X) @ soft_ref.f64(W).T
+    want = s.max(1) - s[np.arange(n), soft_ref.f64(item).astype(int)]
+    bound = (K + 16) * 4 * soft_ref.U * np.abs(s).max(1)  # all products of one sign: |x||w| is |s|
+    with soft.PsSoft(M, K, splits=splits) as h:
+        out = h.xent(X, W, item, grad=grad)
+    if grad:  # rows' weights agree with their own scores, whatever these are off by
+        assert torch.isfinite(out[2]).all()
+    for part, got, v in (("loss", out[0], want), ("lse", out[1], s.max(1))):
+        most = float((np.abs(soft_ref.f64(got) - v) / bound).max())
+        say(f"far below zero splits={splits} grad={grad} {part}: {most:.3f} of its bound")
+        assert most <= 1
