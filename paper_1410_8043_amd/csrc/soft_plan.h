@@ -214,7 +214,7 @@ inline TopPlan top_plan(const Shape *h, int64_t n, int32_t k, bool exclude, int3
     p.bits = a.take(exclude ? p.rows * p.words * 4 : 0);
   } else {
     p.groups = static_cast<int32_t>(up(h->items, kTopGroup));
-    p.rows = std::min(all, std::max<int64_t>(1, (1LL << 30) / (p.groups * (kTopGroup + 1) * 8LL)));
+    p.rows = std::min(all, std::max<int64_t>(1, (1LL << 30) / (8LL * p.groups * (kTopGroup + 1))));
     p.rows = std::min<int64_t>(p.rows, 32768);  // rows are the launch's second dimension
     p.key = a.take(p.rows * p.groups * kTopGroup * 8);
     p.maxima = a.take(p.rows * p.groups * 8);
