@@ -251,3 +251,36 @@ def test_scores_far_below_zero(soft, splits, grad):
         most = float((np.abs(soft_ref.f64(got) - v) / bound).max())
         say(f"far below zero splits={splits} grad={grad} {part}: {most:.3f} of its bound")
         assert most <= 1
+
+
+@pytest.mark.parametrize("M", [33_554_432 + 100, 40_000, 32_700])
+def test_every_record_of_a_list_counts_once(soft, M):
+    # tiles of items that take three sorting passes (from 2^20 tiles on), two, and one; items in every row's list, items of one row,
+    # lists that no item of which is another row's.  A record lost, taken twice or moved is at least 1/200 of an item's sum
+    n, K, per = 40, 1, 3000
+    g = torch.Generator(device="cuda").manual_seed(M)
+    X = (torch.randint(1, 4, (n, K), generator=g, device="cuda") / 4).float()
+    W = torch.randint(-2, 3, (M, K), generator=g, device="cuda").float()
+    item = torch.randint(0, M, (n, per), generator=g, device="cuda", dtype=torch.int32)
+    item[:, 5] = M - 1
+    item[:, 77] = M // 2
+    item[:, 2000:2040] = torch.arange(40, device="cuda").int() * (M // 40)
+    value = torch.randint(1, 6, (n, per), generator=g, device="cuda").float()
+    ptr = torch.arange(0, per * n + 1, per, device="cuda")
+    say(f"records M={M}")
+    with soft.PsSoft(M, K) as h:
+        dW = h.xent(X, W, item.flatten(), row_ptr=ptr, value=value.flatten(), grad="W")[3]
+        again = h.xent(X, W, item.flatten(), row_ptr=ptr, value=value.flatten(), grad="W")[3]
+    assert torch.equal(dW, again)
+    del again
+    x, w = X[:, 0].double(), W[:, 0].double()
+    want, size = torch.zeros(M, dtype=torch.float64, device="cuda"), torch.zeros(M, dtype=torch.float64, device="cuda")
+    for i in range(n):
+        part = value[i].double().sum() * torch.softmax(x[i] * w, 0) * x[i]
+        want += part
+        size += part.abs()
+        want.index_add_(0, item[i].long(), -value[i].double() * x[i])
+        size.index_add_(0, item[i].long(), value[i].double() * x[i])
+    # scores and values are exact; a weight is off by 2^-20 (exponential, log-sum-exp, planes), a sum of n weights and of a
+    # list's records in it by n u
+    assert float(((dW[:, 0].double() - want).abs() / size).max()) <= 2.0 ** -19 + n * soft_ref.U
