@@ -153,6 +153,15 @@ class PsSoft:
             raise ValueError(f"{name} must have shape {tuple('any' if s is None else s for s in shape)}, not {tuple(t.shape)}")
         return t if t.is_contiguous() else t.contiguous()
 
+    @staticmethod
+    def _no_graph(**tensors):
+        """Refuse what autograd would take for a constant without a word."""
+        if torch.is_grad_enabled():
+            for name, t in tensors.items():
+                if isinstance(t, torch.Tensor) and t.requires_grad:
+                    raise ValueError(f"{name} requires a gradient, which autograd does not get from this call: pass {name}.detach(), or call "
+                                     "under torch.no_grad(), and use the gradients that the call returns")
+
     def _on_stream(self):
         s = torch.cuda.current_stream(self.device).cuda_stream
         if s != self._stream:
@@ -185,8 +194,10 @@ class PsSoft:
         ``item`` int32: one target per row [n], or with ``row_ptr`` int64 [n + 1] the entries of row i
         at row_ptr[i] .. row_ptr[i + 1], with ``value`` fp32 (None: 1) each; an item < 0 is none.  ``weight`` fp32
         [n] (None: 1) weights the rows in the gradients; rows without target or of weight 0 are masked.
-        Returns (loss [n], lse [n]) and with ``grad`` (True, or 'X' / 'W' for one of them) also dX, dW.
+        Returns (loss [n], lse [n]) and with ``grad`` (True, or 'X' / 'W' for one of them) also dX, dW.  Autograd does not
+        see the call: tensors that require gradients are refused unless it is off.
         """
+        self._no_graph(X=X, W=W, value=value, weight=weight)
         X, ldx = self._table("X", X, None)
         W, ldw = self._table("W", W, self.items)
         n = X.shape[0]
@@ -208,8 +219,9 @@ class PsSoft:
 
         ``item`` int32 and ``score`` fp32 [n, k]: the teacher's items and its scores of them; an item < 0 or a
         score of -inf is no entry.  ``tlse`` fp32 [n]: the teacher's log-sum-exp of score / tau over all its items (None:
-        its softmax is over the k).  ``weight`` and ``grad`` and the returned values are those of ``xent``.
+        its softmax is over the k).  ``weight``, ``grad``, the returned values and what is said of autograd are those of ``xent``.
         """
+        self._no_graph(X=X, W=W, score=score, tlse=tlse, weight=weight)
         X, ldx = self._table("X", X, None)
         W, ldw = self._table("W", W, self.items)
         n = X.shape[0]
@@ -232,7 +244,7 @@ class PsSoft:
     def top(self, X, W, k, *, row_ptr=None, item=None):
         """The k items of the largest scores of each row, in order, without those that the row excludes (entries
         row_ptr[i] .. row_ptr[i + 1] of ``item``).  Returns (items int32 [n, k], scores fp32 [n, k]); item -1 and
-        score -inf where fewer are left."""
+        score -inf where fewer are left.  The scores carry no gradient."""
         X, ldx = self._table("X", X, None)
         W, ldw = self._table("W", W, self.items)
         n = X.shape[0]
