@@ -286,14 +286,16 @@ int ps_mf_loss_noalloc(ps_mf_t *h, double *out);
    among all items): sum over every loaded rating of D_ij (lse_i - L_i . R_j), lse_i the log-sum-exp of
    L_i . R_j over all items; users without rating add nothing.  A user's part in fp32, their sum in
    fp64 in user order.  Runs on the operators of ps_soft.h; the first call lays the ratings out by
-   user, and the workspace is kept until the handle is destroyed.  Synchronizes. */
+   user, and the workspace is kept until the handle is destroyed.  EINVAL above 2^31 - 65 ratings or
+   items, which those operators do not take.  Synchronizes. */
 int ps_mf_softmax_loss(ps_mf_t *h, double *out);
 
 /* The k items of the largest L_i . R_j at the latest version for n users, 1 <= k <= 256: host arrays
    items and scores (n x k), by decreasing score, equal ones by increasing item; the order is that of
    64-bit sums.  users[n] lists the users (any order, repeats allowed; EINVAL for one out of range),
    NULL: all of them, n = the handle's.  exclude_rated != 0 leaves out the items that the user rated;
-   where fewer than k are left: item -1, score -INFINITY.  Synchronizes. */
+   where fewer than k are left: item -1, score -INFINITY.  EINVAL above 2^31 - 65 items, or excluded
+   ratings of a call.  Synchronizes. */
 int ps_mf_top_items(ps_mf_t *h, const int32_t *users, int64_t n, int32_t k, int32_t exclude_rated, int32_t *items,
                     float *scores);
 

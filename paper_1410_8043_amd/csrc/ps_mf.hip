@@ -3253,9 +3253,15 @@ int soft_fail(ps_mf_t *h, int rc) {  // the codes are the same
 
 int soft_open(ps_mf_t *h) {
   if (!h->soft) {
-    const int rc = ps_soft_create(h->M, h->K, PS_SOFT_F32, &h->soft);
+    ps_soft_t *soft = nullptr;
+    int rc = ps_soft_create(h->M, h->K, PS_SOFT_F32, &soft);
     if (rc) return fail(h, rc, "the operators over %lld items of rank %d", (long long)h->M, h->K);
-    if (const int r = ps_soft_set_option(h->soft, PS_SOFT_OPT_DEVICE, h->device)) return soft_fail(h, r);
+    if ((rc = ps_soft_set_option(soft, PS_SOFT_OPT_DEVICE, h->device))) {
+      fail(h, rc, "%s", ps_soft_last_error(soft));
+      ps_soft_destroy(soft);  // one without its device would use the current one
+      return rc;
+    }
+    h->soft = soft;
   }
   return soft_fail(h, ps_soft_set_stream(h->soft, h->stream));
 }
