@@ -966,16 +966,19 @@ __global__ __launch_bounds__(kSumThreads) void k_sum_rows(const float *__restric
   if (threadIdx.x == 0) *out = sh[0];
 }
 
-// One block's lists by user to their places among all blocks' (a wavefront per user)
+// One block's lists by user to their places among all blocks' (a wavefront per user, users in turn: a launch holds
+// less than 2^32 threads)
+constexpr int64_t kListBlocks = 1 << 16;
 __global__ __launch_bounds__(kBlock) void k_copy_lists(int64_t n, const int64_t *__restrict__ from, const int32_t *__restrict__ col,
                                                        const float *__restrict__ val, const int64_t *__restrict__ to,
                                                        int32_t *__restrict__ item, float *__restrict__ out) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64;
-  if (i >= n) return;
-  const int64_t b = from[i], len = from[i + 1] - b, t = to[i];
-  for (int64_t q = threadIdx.x & 63; q < len; q += 64) {
-    item[t + q] = col[b + q];
-    out[t + q] = val[b + q];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * (kBlock / 64);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + threadIdx.x / 64; i < n; i += step) {
+    const int64_t b = from[i], len = from[i + 1] - b, t = to[i];
+    for (int64_t q = threadIdx.x & 63; q < len; q += 64) {
+      item[t + q] = col[b + q];
+      out[t + q] = val[b + q];
+    }
   }
 }
 
@@ -3291,7 +3294,8 @@ int merge_block(ps_mf_t *h, int b, std::vector<int64_t> &from, std::vector<int64
   if ((r = buffer(h, d_to, n * 8)) || (r = buffer(h, d_from, (n + 1) * 8))) return r;
   HIP_TRY(h, hipMemcpyAsync(d_to.p, to.data(), n * 8, hipMemcpyHostToDevice, h->stream));
   HIP_TRY(h, hipMemcpyAsync(d_from.p, from.data(), (n + 1) * 8, hipMemcpyHostToDevice, h->stream));
-  hipLaunchKernelGGL(k_copy_lists, dim3(static_cast<unsigned>((n + 3) / 4)), dim3(kBlock), 0, h->stream, static_cast<int64_t>(n),
+  const unsigned blocks = static_cast<unsigned>(std::min(static_cast<int64_t>((n + 3) / 4), kListBlocks));
+  hipLaunchKernelGGL(k_copy_lists, dim3(blocks), dim3(kBlock), 0, h->stream, static_cast<int64_t>(n),
                      static_cast<const int64_t *>(d_from.p), h->dblocks[b].col, h->dblocks[b].val, static_cast<const int64_t *>(d_to.p),
                      static_cast<int32_t *>(h->all_item.p), static_cast<float *>(h->all_val.p));
   HIP_TRY(h, hipGetLastError());
