@@ -43,7 +43,8 @@
  *   - the losses scale each table by a power of two and round its numbers: fp32 to 22 bits, but to no
  *     less than 2^-38 of the table's largest finite number (felt below 2^-16 of it; bf16 and f16
  *     numbers are exact above 2^-28 of it).  The softmax's weights have 22 bits, those of a row or of an
- *     item that are far below its largest to 2^-31 of that one;
+ *     item that are far below its largest to 2^-31 of that one (an item's beside targets: to 2^-38 of
+ *     the sum of these);
  *     A score is off by about 2^-22 of sum |x_k w_k|: where that is no longer small against 1 (scores
  *     beyond 10^5), gradients lose their digits, and dW its meaning (beyond 10^7);
  *   - equal calls give equal bits: sums have a fixed order, whatever runs beside them.

@@ -522,6 +522,9 @@ __device__ inline int64_t first_of_row(const uint2 *pay, int64_t b, int64_t e, u
   return b;
 }
 
+// What targets are multiplied by for their place beside weights of that reference; any finite number where there are none
+__device__ inline float up_to(float ref) { return __builtin_amdgcn_exp2f(fminf(kShift - ref, kShift - kFar)); }
+
 // The largest of the two lanes that hold an own row
 __device__ inline float of_both_halves(float v) {
   const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -584,22 +587,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   auto fetch_rows = [&](int t) {
     if (COL && wave == 0) to_lds4(a.rowvec + static_cast<int64_t>(t) * 64 + lane, buf + sg.at_rows + (t & 3) * 128);
   };
-  h8 q[KC][NP];
-  const _Float16 *own = a.own + own_tile * a.own_stride;
-#pragma unroll
-  for (int c = 0; c < KC; ++c)
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      q[c][p] = h8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (live) q[c][p] = *reinterpret_cast<const h8 *>(own + (c * NP + p) * kFrag + lane * 8);
-    }
-  f32x16 o[DB > 0 ? DB : 1];
-#pragma unroll
-  for (int b = 0; b < DB; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-  // The reference of each own row follows the largest of its own weights, an item's targets among them: so an item of
-  // small weights keeps 22 bits of them, whatever its neighbours' or the rows' shares are.
+  // The reference of each own row follows the largest of its own weights, and an item's starts where all of its targets in this
+  // piece together are 2^14 at most: so an item of small weights keeps 22 bits of them, whatever its neighbours' or the rows' shares
+  // are.  (Asking each half tile's targets for their largest instead took 4 to 18% of a call.)
   float ref = kNone, sum = 0.f, lost = 0.f, unit = 0.f;
   bool targets = false;
   Window win;
@@ -614,8 +604,46 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       win.open(a.pay, b, e, lane);
       targets = win.due < static_cast<uint32_t>(t1) * kTile;
     }
-    unit = 1.f / a.scal->amax;
+    if (targets) {
+      unit = 1.f / a.scal->amax;
+      // by item, 16 sums each so that few lanes meet at one
+      const int64_t e = a.first[own_tile + 1];
+      bool more = true;
+      for (int64_t at = win.pay - a.pay + lane; more; at += 256) {
+        uint2 r[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) r[u] = at + 64 * u < e ? a.pay[at + 64 * u] : make_uint2(0xffffffffu, 0u);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          more = (r[u].x >> 5) < static_cast<uint32_t>(t1) * kTile;
+          if (more) atomicAdd(y + (r[u].x & 31) * 16 + (lane & 15), fabsf(__uint_as_float(r[u].y)) * unit);
+        }
+        more = __any(more);
+      }
+      __builtin_amdgcn_wave_barrier();
+      f32x4 *const mine = reinterpret_cast<f32x4 *>(y + (lane & 31) * 16);
+      const f32x4 v = (mine[0] + mine[1]) + (mine[2] + mine[3]);
+      __builtin_amdgcn_wave_barrier();
+      mine[0] = mine[1] = mine[2] = mine[3] = f32x4{0.f, 0.f, 0.f, 0.f};
+      __builtin_amdgcn_wave_barrier();
+      const float all = (v[0] + v[1]) + (v[2] + v[3]);
+      if (all > 0.f) ref = fmaxf(__builtin_amdgcn_logf(all) - (14.f - kShift), kFar);
+    }
   }
+  h8 q[KC][NP];
+  const _Float16 *own = a.own + own_tile * a.own_stride;
+#pragma unroll
+  for (int c = 0; c < KC; ++c)
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      q[c][p] = h8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (live) q[c][p] = *reinterpret_cast<const h8 *>(own + (c * NP + p) * kFrag + lane * 8);
+    }
+  f32x16 o[DB > 0 ? DB : 1];
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
   // Chunk c of a tile's score fragments, and step i of its turned ones (half i / DB, block i % DB)
   auto read_scores = [&](h8 (&f)[NP], int t, int c) {
     const _Float16 *from = buf + (sg.score_tiles == 2 ? (t & 1) * sg.scores * kFrag : 0) + c * NP * kFrag + lane * 8;
@@ -778,24 +806,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
             __builtin_amdgcn_wave_barrier();
             *y0 = *y1 = f32x4{0.f, 0.f, 0.f, 0.f};
             __builtin_amdgcn_wave_barrier();
-            // as the weights', and half of their room: the two together stay below 2^15 + 2^14
-            float big = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fabsf(v0[i]), fabsf(v1[i])));
-            big = of_both_halves(big);
-            float to = big > 0.f ? fmaxf(ref, kFar) : ref;
-            if (big > __builtin_amdgcn_exp2f(to + (kLag - 1.f))) to = __builtin_amdgcn_logf(big);
-            if (__any(to != ref)) {
-              const float down = __builtin_amdgcn_exp2f(ref - to);
-              ref = to;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) p[r] *= down;
-#pragma unroll
-              for (int b = 0; b < DB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[b][r] *= down;
-            }
-            const float up = __builtin_amdgcn_exp2f(fminf(kShift - ref, kShift - kFar));  // lanes without targets: any finite number
+            const float up = up_to(ref);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               p[8 * k + i] = fmaf(-up, v0[i], p[8 * k + i]);

@@ -284,3 +284,30 @@ def test_every_record_of_a_list_counts_once(soft, M):
     # scores and values are exact; a weight is off by 2^-20 (exponential, log-sum-exp, planes), a sum of n weights and of a
     # list's records in it by n u
     assert float(((dW[:, 0].double() - want).abs() / size).max()) <= 2.0 ** -19 + n * soft_ref.U
+
+
+@pytest.mark.parametrize("splits", [0, 2])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_a_row_that_lists_an_item_thousands_of_times(soft, dtype, splits):
+    # and a popular item beside it, and neighbours of either that hardly any row wants
+    n, M, K, times = 70, 64, 6, 3000
+    X, W, g = tables(n, M, K, dtype, 11)
+    X[:, 0] = 4
+    W[:, 0] = 0
+    W[20:30, 0] = -4
+    lists = [[int(j)] for j in torch.randint(0, M, (n,), generator=g)]
+    for i in range(n):
+        lists[i].append(22)
+    lists[40] = [7] * times
+    y = np.zeros((n, M))
+    for i, l in enumerate(lists):
+        np.add.at(y[i], l, 1.0)
+    ptr = torch.tensor(np.cumsum([0] + [len(l) for l in lists])).cuda()
+    item = torch.tensor([j for l in lists for j in l], dtype=torch.int32).cuda()
+    weight = torch.full((n,), 2.0 ** -8)
+    want, bound = item_gradients(soft_ref.f64(X), soft_ref.f64(W), y, soft_ref.f64(weight))
+    with soft.PsSoft(M, K, dtype, splits=splits) as h:
+        got = h.xent(X, W, item, row_ptr=ptr, weight=weight.cuda())[3]
+    most = off(got, want, bound, dtype)
+    say(f"thousands of times {dtype} splits={splits}: {most:.3f} of its bound")
+    assert most <= 1
