@@ -72,9 +72,11 @@ inline int32_t padded_chunks(int32_t K) {
 inline int32_t pieces(int64_t own_tiles, int64_t tiles, int32_t forced) {
   const int64_t groups = up(own_tiles, kWaves);
   if (forced > 0) return static_cast<int32_t>(std::max<int64_t>(1, std::min({static_cast<int64_t>(forced), tiles, (static_cast<int64_t>(1) << 30) / groups})));
-  // many own rows: a piece more costs its part of the join (782 workgroups of 100,000 items: 8 pieces 1292 us and 190 of
-  // joining, 4 pieces 1274 and 95, 2 pieces 1387 and 48)
-  if (groups >= 512) return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(tiles / 8, groups >= 4096 ? 1 : groups >= 2048 ? 2 : 4)));
+  // 512 workgroups run at once.  Up to two rounds of them 4 pieces fill the last round (550 workgroups of K = 128 fp32, 8192 streamed
+  // rows: 1 piece 917 us with the join, 2 801, 4 765, 8 824; 782: 1218, 1133, 1108, 1156); from there on the rounds are
+  // many and a piece more only costs its part of the join (1000, K = 128 bf16, 4096 rows: 391, 406, 445, 530; 2200: 889, 921,
+  // 997, 1208; 4500: 1771, 1843, 2030, 2418).  Longer streams differ less (1000, 32,768 rows: 2942, 2929, 2949, 3025)
+  if (groups >= 512) return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(tiles / 8, groups >= 1000 ? 1 : 4)));
   const int64_t most = std::max<int64_t>(1, groups * (tiles / 8) < 256 ? std::min(up(256, groups), tiles / 2) : tiles / 8);
   int64_t want = up(768, groups);
   if (most >= 8) want = up(want, 8) * 8;
