@@ -331,8 +331,8 @@ struct PackSide {
 // 16c + 8(l/32) ..+7; and turned, for the sums, rows 16q ..+15 and numbers 32b ..+31: lane l holds
 // number 32b + l%32 of the rows that the score instruction leaves in this lane's registers
 // 8q .. 8q+7, 16q + {4h ..+3, 8 + 4h ..+3} with h = l/32: so weights go from one matrix instruction to
-// the next without a move.  One workgroup per tile; bound by memory (8192 + 100,000 rows, K = 256 bf16: 165 MB in 31 us,
-// 5.3 TB/s).
+// the next without a move.  One workgroup per tile; bound by memory (8192 + 100,000 rows, K = 256 bf16: 165 MB in 32 us,
+// 5.2 TB/s).
 template <class T, int NP>
 __global__ __launch_bounds__(kThreads) void k_pack(Table<T> x, Table<T> w, PackSide px, PackSide pw, int32_t K, int32_t k16,
                                                    int32_t kd, const float *part, const float *row_part, int32_t row_parts,
@@ -543,11 +543,12 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // 8(r/4) + 4h + r%4 of each tile.
 // The weights have two planes whatever the tables' type: with one, 2^-11 of each weight, 6 of 100 numbers of a bf16
 // gradient are rounded to the neighbour of the nearest.
-// The matrix instructions bound rows over items (1.16 PFLOP/s of them at K = 128 fp32, 1.14 at K = 256 bf16; a large
+// The matrix instructions bound rows over items (1.11 PFLOP/s of them at K = 128 fp32, 1.11 at K = 256 bf16; a large
 // library product reaches 1.2), so the loop keeps them fed: the next tile's scores are made beside the exponentials of this one's,
-// the sums beside the rounding.  Items over rows have the records and the factors besides (K = 128 fp32 385 / 510 us).  The
-// tiles' way from L2 is a seventh to a fifth of it: 8 wavefronts a workgroup, which halve that, 320 / 360 us for 331 / 316; two own tiles a
-// wavefront, which halve the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
+// the sums beside the rounding.  Items over rows have the records and the factors besides (16,384 rows x 17,770 items, K = 128
+// fp32, 403 / 562 us; 4096 x 100,000, K = 128 bf16, 332 / 396).  The tiles' way from L2 is a seventh to a fifth of it.  With items' weights of
+// one plane (331 / 316 us then) were tried: 8 wavefronts a workgroup, which halve that way, 320 / 360; two own tiles a wavefront, which halve
+// the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
 template <int NP, int KC, int DB, bool COL>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pass(PassArgs a) {
   constexpr Stage sg = stage_of(NP, KC, DB, COL);
@@ -907,7 +908,7 @@ struct RowArgs {
 
 // TW wavefronts per row (more for few rows).  The targets' part is c_i = sum coef w_j: dX_i needs it, and the loss
 // too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it
-// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 212 us, 8.2 TB/s, 58% of it from L2).
+// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 209 us, 8.4 TB/s, 58% of it from L2).
 template <class T, int G, int V, int TW>
 __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowArgs<T> a) {
   constexpr int NG = TW * 64 / G;      // groups per row
@@ -1362,7 +1363,7 @@ struct ItemArgs {
   bool vec_out;
 };
 
-// dW_j: the passes' pieces joined.  Bound by memory (100,000 items in 4 pieces, K = 256 bf16: 461 MB in 100 us, 4.6 TB/s).
+// dW_j: the passes' pieces joined.  Bound by memory (100,000 items in 4 pieces, K = 256 bf16: 461 MB in 95 us, 4.9 TB/s).
 template <class T, int G, int V>
 __global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
   const int g = threadIdx.x & (G - 1);
