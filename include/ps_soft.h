@@ -45,8 +45,8 @@
  *     numbers are exact above 2^-28 of it).  The softmax's weights have 22 bits, those of a row or of an
  *     item that are far below its largest to 2^-31 of that one (an item's beside targets: to 2^-38 of
  *     the sum of these);
- *     A score is off by about 2^-22 of sum |x_k w_k|: where that is no longer small against 1 (scores
- *     beyond 10^5), gradients lose their digits, and dW its meaning (beyond 10^7);
+ *     A score is off by about 2^-22 of sum |x_k w_k|, in the same way for rows and items: beyond 10^5 that
+ *     is felt where several items share a row's softmax, and dW loses its meaning beyond 10^7;
  *   - equal calls give equal bits: sums have a fixed order, whatever runs beside them.
  */
 #ifndef PS_SOFT_H

@@ -320,6 +320,9 @@ struct Scal {
 };
 static_assert(sizeof(Scal) == kScalBytes, "the workspace's plan");
 
+// log2 of the weights per unit of the packed tables' scores; scale: log2(e) / tau.  Not 0, so that -inf stays
+__device__ inline float unit_of(const Scal *scal, float scale) { return fmaxf(ldexpf(scale, -(scal->ex + scal->ew)), 0x1p-126f); }
+
 struct PackSide {
   _Float16 *out;
   int64_t stride;  // halves per tile
@@ -413,7 +416,7 @@ struct PassArgs {
   int64_t tiles_per_split;
   const int64_t *first;            // COL: where the records of each own tile start ([own tiles + 1], NULL: none)
   const uint2 *pay;                // sorted by own tile, then row
-  float *m, *l, *o;                // [splits][own rows padded]: reference, sum of p', sums [..][32 kd]
+  float *m, *l, *o;                // [splits][own rows padded]: reference (COL: in powers of two; else a packed tables' score), sum of p', sums [..][32 kd]
 };
 
 __device__ inline f32x16 mfma(h8 a, h8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -563,7 +566,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   const int64_t tiles = (a.str_rows + kTile - 1) / kTile;
   const int t0 = static_cast<int>(split * a.tiles_per_split);
   const int t1 = static_cast<int>(min(t0 + a.tiles_per_split, tiles));
-  const float sc = ldexpf(a.scale, -(a.scal->ex + a.scal->ew));
+  const float sc = unit_of(a.scal, a.scale);
   const bool live = own_tile < a.own_tiles;  // the last workgroup's wavefronts behind the last row only help loading
   auto fetch_scores = [&](int t) {
     const _Float16 *src = a.str + t * a.str_stride + lane * 8;
@@ -656,16 +659,20 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
 #pragma unroll
     for (int p = 0; p < NP; ++p) f[p] = *reinterpret_cast<const h8 *>(from + p * kFrag);
   };
+  // An item's and a row's planes in the same order in both passes, so a score has equal bits in them: a weight that is nearly 1 in
+  // the row's sum is that in the item's difference to its target
   auto add_scores = [&](f32x16 s, const h8 (&f)[NP], int c) {
     s = mfma(f[0], q[c][0], s);
     if constexpr (NP == 2) {
-      s = mfma(f[0], q[c][1], s);
-      s = mfma(f[1], q[c][0], s);
+      s = mfma(f[COL], q[c][!COL], s);
+      s = mfma(f[!COL], q[c][COL], s);
     }
     return s;
   };
-  // log2 weights of stream rows r: the score's, and the row's power of two.  That is added here: as the matrix
-  // instruction's first value, every one of its roundings would be at the size of the log-sum-exp
+  // Rows over items: the scores as they are, and the reference one of them, so that what the exponential gets is rounded at the
+  // size of their difference (scaled scores rounded at their own size left weights near 1 2^-25 |score| off, and with them
+  // the items' differences to their targets).  Items over rows: log2 weights, the score's and the row's power of two.  That is
+  // added here: as the matrix instruction's first value, every one of its roundings would be at the size of the log-sum-exp
   auto row_values = [&](int t, int g, int which) {  // rows 8g + 4h ..+3: the powers of two, or the factors
     return *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(buf + sg.at_rows + (t & 3) * 128) + which * 32 + g * 8 + half * 4);
   };
@@ -679,12 +686,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   float p[16], top;
+  const float lag = COL ? kLag : kLag / sc;
   auto weigh = [&](const f32x16 &s, int t) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 v = COL ? row_values(t, g, 0) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * g + i] = COL ? fmaf(s[4 * g + i], sc, v[i]) : s[4 * g + i] * sc;
+      for (int i = 0; i < 4; ++i) p[4 * g + i] = COL ? fmaf(s[4 * g + i], sc, v[i]) : s[4 * g + i];
     }
     top = p[0];
 #pragma unroll
@@ -730,9 +738,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       }
     }
     top = of_both_halves(top);
-    if (__any(top > ref + kLag)) {
-      const float to = top > ref + kLag ? top : ref;
-      const float down = __builtin_amdgcn_exp2f(ref - to);
+    if (__any(top > ref + lag)) {
+      const float to = top > ref + lag ? top : ref;
+      const float down = __builtin_amdgcn_exp2f(COL ? ref - to : (ref - to) * sc);
       ref = to;
       sum *= down;
       lost *= down;
@@ -760,7 +768,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
       next = add_scores(next, f[c], c);
 #pragma unroll
       for (int r = 16 * c / KC; r < 16 * (c + 1) / KC; ++r) {
-        p[r] = __builtin_amdgcn_exp2f(p[r] + shift);
+        p[r] = __builtin_amdgcn_exp2f(COL ? p[r] + shift : fmaf(p[r] - ref, sc, kShift));
         if constexpr (COL) p[r] *= factor[r >> 2][r & 3];
         else w[r & 3] += p[r];
         asm volatile("" : "+v"(p[r]));  // here, beside the matrix instructions
@@ -850,7 +858,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(NP, KC, DB)) void k_pas
         }
 #pragma unroll
         for (int r = 16 * i / (2 * DB); r < 16 * (i + 1) / (2 * DB); ++r) {
-          n[r] = COL ? fmaf(next[r], sc, v[r >> 2][r & 3]) : next[r] * sc;
+          n[r] = COL ? fmaf(next[r], sc, v[r >> 2][r & 3]) : next[r];
           m[r & 1] = fmaxf(m[r & 1], n[r]);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -898,6 +906,7 @@ struct RowArgs {
   int32_t K, ldo, splits;
   Table<T> x, w;
   const Scal *scal;
+  float scale;             // log2(e) / tau; 0: the references are powers of two (k_few's)
   const float *m, *l, *o;
   float *loss, *lse;
   T *dX;
@@ -928,19 +937,20 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     return;
   }
   const bool act = a.t.act[i];
+  const float unit = a.scale > 0.f ? unit_of(a.scal, a.scale) : 1.f;
   float top = kNone, den = 0.f;
 #pragma unroll 4
   for (int s = lane; s < a.splits; s += 64) {
     const float m = a.m[s * a.own_pad + i], l = a.l[s * a.own_pad + i];
     const float now = fmaxf(top, m);
-    den = den * __builtin_amdgcn_exp2f(top - now) + l * __builtin_amdgcn_exp2f(m - now);
+    den = den * __builtin_amdgcn_exp2f((top - now) * unit) + l * __builtin_amdgcn_exp2f((m - now) * unit);
     top = now;
   }
   const float mine = top;
   top = wave_max(top);
-  den = wave_sum(den * __builtin_amdgcn_exp2f(mine - top));
+  den = wave_sum(den * __builtin_amdgcn_exp2f((mine - top) * unit));
   // in 64 bits: the loss is what is left of total lse - x . c, and a log2-sum-exp in 32 would be off by 5e-7 at 8 .. 16
-  const double lse64 = static_cast<double>(top) - static_cast<double>(kShift) + log2(static_cast<double>(den)), lse = lse64 * 0.69314718055994530942;
+  const double lse64 = static_cast<double>(top) * unit - static_cast<double>(kShift) + log2(static_cast<double>(den)), lse = lse64 * 0.69314718055994530942;
   f32x4 acc[V], o[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -985,7 +995,7 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
     }
     if (a.dX)
       for (int s = grp; s < a.splits; s += NG) {
-        const float f = __builtin_amdgcn_exp2f(a.m[s * a.own_pad + i] - top);
+        const float f = __builtin_amdgcn_exp2f((a.m[s * a.own_pad + i] - top) * unit);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int k0 = v * 4 * G + 4 * g;
@@ -1048,8 +1058,9 @@ __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowAr
       const double v = (m == 0.f ? -__builtin_inf() : static_cast<double>(e)) - lse64;
       const float v32 = static_cast<float>(v);
       a.rowvec[(i >> 5) * 64 + (i & 31)] = act ? v32 : -__builtin_inff();
-      const double rest = (v - v32) * 0.69314718055994530942;  // below 2^-9 for scores below 2^15
-      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = m == 0.f ? 0.f : m * static_cast<float>(1.0 + rest * (1.0 + 0.5 * rest));
+      const double rest = (v - v32) * 0.69314718055994530942;  // below 2^-9 for scores below 2^15, and 2^-3 below 2^21
+      const double back = 1.0 + rest * (1.0 + rest * (1.0 / 2 + rest * (1.0 / 6 + rest * (1.0 / 24))));
+      a.rowvec[(i >> 5) * 64 + 32 + (i & 31)] = m == 0.f ? 0.f : m * static_cast<float>(back);
     }
   }
   if (a.dX && lane < G) {
@@ -2261,6 +2272,7 @@ int soft_loss(ps_soft_t *h, Targets t, const T *X, int64_t ldx, const T *W, int6
     r.x = x;
     r.w = w;
     r.scal = scal;
+    r.scale = p.few ? 0.f : scale;
     r.m = a.m;
     r.l = a.l;
     r.o = a.o;

@@ -311,3 +311,39 @@ def test_a_row_that_lists_an_item_thousands_of_times(soft, dtype, splits):
     most = off(got, want, bound, dtype)
     say(f"thousands of times {dtype} splits={splits}: {most:.3f} of its bound")
     assert most <= 1
+
+
+@pytest.mark.parametrize("splits", [0, 3])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("size", [30.0, 1e3, 3e4, 1e6])
+def test_confident_rows_of_large_scores(soft, size, dtype, splits):
+    # a row's target takes its whole softmax: what is left of p - 1 may not depend on how large the scores are.  A score's error e
+    # moves p to at most p / (p + (1 - p) exp(+-2 e)); the exponentials, log-sum-exps and planes are 2^-20, sums 2 u a term
+    n, M, K = 200, 220, 32
+    W, g = torch.randn(M, K, generator=torch.Generator().manual_seed(int(size))), torch.Generator().manual_seed(3)
+    scale = (size / K) ** 0.5
+    X = (W[:n] * (1 + 0.02 * torch.randn(n, K, generator=g)) * scale).to(dtype).cuda()
+    W = (W * scale).to(dtype).cuda()
+    item = torch.arange(n).int()
+    item[::16] += 5
+    x, w = soft_ref.f64(X), soft_ref.f64(W)
+    s, a = x @ w.T, np.abs(x) @ np.abs(w).T
+    top = s.max(1, keepdims=True)
+    e = np.exp(s - top)
+    p, rest = e / e.sum(1, keepdims=True), np.empty_like(e)
+    for j in range(M):  # 1 - p without cancellation
+        rest[:, j] = np.delete(e, j, 1).sum(1) / e.sum(1)
+    y = np.zeros((n, M))
+    y[np.arange(n), item] = 1
+    want = (p - y).T @ x
+    es = np.minimum((K + 16) * 2 * soft_ref.U * a.max(1, keepdims=True), 300)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        up = p / (p + rest * np.exp(-2 * es)) - p
+        down = p - p / (p + rest * np.exp(2 * es))
+    moved = np.where(p > 0, np.maximum(np.abs(np.nan_to_num(up)), np.abs(np.nan_to_num(down))), 0)
+    bound = (moved + p * (2.0 ** -20 + 2 * (M + 16) * soft_ref.U) + y * (n + 16) * soft_ref.U + 2.0 ** -31).T @ np.abs(x)
+    with soft.PsSoft(M, K, dtype, splits=splits) as h:
+        got = h.xent(X, W, item.cuda())
+    most = off(got[3], want, bound, dtype)
+    say(f"confident size={size} {dtype} splits={splits}: {most:.3f} of its bound")
+    assert most <= 1 and torch.isfinite(got[2]).all()
