@@ -546,10 +546,10 @@ constexpr int waves_per_simd(int np, int kc, int db) {
 // 8(r/4) + 4h + r%4 of each tile.
 // The weights have two planes whatever the tables' type: with one, 2^-11 of each weight, 6 of 100 numbers of a bf16
 // gradient are rounded to the neighbour of the nearest.
-// The matrix instructions bound rows over items (1.11 PFLOP/s of them at K = 128 fp32, 1.11 at K = 256 bf16; a large
+// The matrix instructions bound rows over items (1.12 PFLOP/s of them at K = 128 fp32, 1.08 at K = 256 bf16; a large
 // library product reaches 1.2), so the loop keeps them fed: the next tile's scores are made beside the exponentials of this one's,
 // the sums beside the rounding.  Items over rows have the records and the factors besides (16,384 rows x 17,770 items, K = 128
-// fp32, 403 / 562 us; 4096 x 100,000, K = 128 bf16, 332 / 396).  The tiles' way from L2 is a seventh to a fifth of it.  With items' weights of
+// fp32, 400 / 557 us; 4096 x 100,000, K = 128 bf16, 337 / 388).  The tiles' way from L2 is a seventh to a fifth of it.  With items' weights of
 // one plane (331 / 316 us then) were tried: 8 wavefronts a workgroup, which halve that way, 320 / 360; two own tiles a wavefront, which halve
 // the reads of LDS too and leave one wavefront a SIMD, 421 / 458; reading further ahead the same.
 template <int NP, int KC, int DB, bool COL>
@@ -917,7 +917,7 @@ struct RowArgs {
 
 // TW wavefronts per row (more for few rows).  The targets' part is c_i = sum coef w_j: dX_i needs it, and the loss
 // too, since sum coef s_ij = x_i . c_i: one product per row instead of one per target.  Gathers of w rows bound it
-// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 209 us, 8.4 TB/s, 58% of it from L2).
+// (16,384 rows of 208 items, K = 128 fp32: 1.75 GB in 212 us, 8.3 TB/s, 58% of it from L2).
 template <class T, int G, int V, int TW>
 __global__ __launch_bounds__(TW == 16 ? 1024 : kThreads) void k_row_finish(RowArgs<T> a) {
   constexpr int NG = TW * 64 / G;      // groups per row
@@ -1374,7 +1374,7 @@ struct ItemArgs {
   bool vec_out;
 };
 
-// dW_j: the passes' pieces joined.  Bound by memory (100,000 items in 4 pieces, K = 256 bf16: 461 MB in 95 us, 4.9 TB/s).
+// dW_j: the passes' pieces joined.  Bound by memory (100,000 items in 4 pieces, K = 256 bf16: 461 MB in 98 us, 4.7 TB/s).
 template <class T, int G, int V>
 __global__ __launch_bounds__(kThreads) void k_item_finish(ItemArgs<T> a) {
   const int g = threadIdx.x & (G - 1);
